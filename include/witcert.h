@@ -74,8 +74,12 @@ enum {
     WC_DEV_TIMEOUT = 8u,      /* decode: a bounded wait for staged data gave up   */
     WC_DEV_BAD_PAIR = 16u,    /* grouped scheme: a bypass pair outside [0, 64), or listed
                                  again, is ignored (its two stored values are 0) */
-    WC_DEV_BAD_APPEND = 32u   /* append: slot_new[b] is not the slot of the context's last
+    WC_DEV_BAD_APPEND = 32u,  /* append: slot_new[b] is not the slot of the context's last
                                  token; the token is not written */
+    WC_DEV_BAD_POSITION = 64u,/* block append: a rotary position outside the tables; the
+                                 token is not written, its rotated query rows are 0 */
+    WC_DEV_BAD_ROWS = 128u    /* block calls: a sequence's token range [cu[b], cu[b + 1]) is not
+                                 an ascending one within [0, n_tok]; the sequence is skipped */
 };
 
 typedef enum {
@@ -469,6 +473,132 @@ wc_status wc_gate(const float* meter_raw, int32_t n_cells, int32_t group, float 
 wc_status wc_gate_joint(const float* meter_raw, const float* value_term, const float* v_max,
                         int32_t n_cells, int32_t group, float tau_k, float tau_v,
                         uint8_t* keep_q, uint8_t* keep_kv, int32_t* n_kept, void* stream);
+
+/*
+ * Block-scaled 8-bit cache (no counterpart in the paper: the unmetered 8-bit
+ * cache of a serving stack, beside the metered one).  One fp32 scale for the 16
+ * tokens of a page and KV head; x^ = scale * code:
+ *   k_codes, v_codes [num_pages][Hkv][16][128]  int8, or fp8 e4m3fn bytes
+ *   k_scale, v_scale [num_pages][Hkv]           fp32, >= 0
+ * The code arrays have the layout of WC_SCHEME_FP8_E4M3's, so the attention
+ * calls below also read that scheme's cache (k_scale = v_scale = NULL: scale 1).
+ */
+typedef enum {
+    /* code = rn(x / scale) in [-127, 127], scale = amax * fp32(1 / 127) */
+    WC_CODE_INT8 = 0,
+    /* code = e4m3 rn(x / scale), scale the least power of two with amax <= 448 scale: a page
+     * whose scale grows then keeps its codes' bits (all but subnormals) */
+    WC_CODE_E4M3 = 1
+} wc_block_code;
+
+/* Element type of k, v, q and the attention's out. */
+typedef enum { WC_ACT_FP16 = 0, WC_ACT_BF16 = 1 } wc_act_type;
+
+typedef struct {
+    int32_t head_dim;       /* must be 128                                        */
+    int32_t num_q_heads;    /* Hq; Hq % Hkv == 0 and Hq / Hkv <= 128               */
+    int32_t num_kv_heads;   /* Hkv, 1 .. 65535                                     */
+    int32_t page_size;      /* must be 16                                          */
+    int32_t num_pages;      /* pages in the layer's pool                           */
+    int32_t code;           /* wc_block_code                                       */
+    int32_t rope_layout;    /* wc_rope_layout                                      */
+    int32_t rotary_dim;     /* leading dims of a head that the append rotates: a multiple of
+                               16 up to 128, 0: none.  WC_ROPE_HALF pairs dims (j, j + rotary_dim / 2),
+                               WC_ROPE_INTERLEAVED (2j, 2j + 1)                     */
+} wc_block_desc;
+
+/*
+ * Appends every sequence's new tokens to a block-scaled cache, rotating keys
+ * (and, if given, queries) to their positions on the way.
+ *
+ * Sequence b's new tokens are rows cu_new[b] .. cu_new[b + 1] - 1 of k, v and q and the
+ * last of its context: logical positions ctx_lens[b] - n_b .. ctx_lens[b] - 1.  In fp32, each
+ * product rounded, pair j of a row at rotary position p becomes
+ *   (x_a cos[p][j] - x_b sin[p][j],  x_b cos[p][j] + x_a sin[p][j]).
+ * For each page and KV head with new tokens, K and V separately:
+ *   s  = scale from amax over the page's new rows (0 if amax is 0, else >= 2^-100),
+ *   s' = max(s, the stored scale) if the page holds older tokens (positions
+ *        below the new ones), else s;
+ *   codes of the new rows are rn(x * fp32(1 / s')), and where s' is above the stored scale
+ *   the older tokens' codes become rn(code * fp32(stored / s')).
+ * What a page holds past the new tokens is left as it is and not looked at, so
+ * a token appended again at an earlier position (a draft that was rejected)
+ * replaces the one that was there.  A row with infinities or NaN makes its page's scale that (sticky until
+ * the page is begun anew) and its codes 0, and attention over the page NaN.
+ * A page written by the call belongs to one sequence (as with wc_metered_decode_attention_append).
+ *
+ *   k, v         [n_tok][Hkv][128] act_type, device; k_stride, v_stride elements from one
+ *                token to the next (>= Hkv * 128, a multiple of 8): views of a packed projection
+ *   q, q_out     [n_tok][Hq][128]; q with q_stride, q_out dense; both NULL: no queries
+ *   cu_new       [batch + 1] int32, ascending, cu_new[batch] <= n_tok; NULL: one token per
+ *                sequence (n_tok = batch)
+ *   block_table  [batch][max_pages] int32; entries past a sequence's pages are not read
+ *   ctx_lens     [batch] int32, with the new tokens
+ *   positions    [n_tok] int32 rotary positions; NULL: the logical positions
+ *   cos_table, sin_table  [num_positions][rotary_dim / 2] fp32; NULL if rotary_dim is 0
+ *   dev_status   optional device uint32: WC_DEV_BAD_PAGE, _CTX (ctx_lens[b] < n_b or past the
+ *                block table; the sequence is skipped), _POSITION, _ROWS
+ */
+wc_status wc_block_append(const wc_block_desc* desc, int32_t act_type,
+                          const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                          const void* q, int64_t q_stride, void* q_out, int32_t n_tok,
+                          const int32_t* cu_new, const int32_t* block_table, int32_t max_pages,
+                          const int32_t* ctx_lens, int32_t batch, const int32_t* positions,
+                          const float* cos_table, const float* sin_table, int32_t num_positions,
+                          void* k_codes, void* v_codes, float* k_scale, float* v_scale,
+                          uint32_t* dev_status, void* stream);
+
+/*
+ * Bytes of workspace the two attention calls need for `batch` sequences with
+ * n_tok query tokens in all (decode: n_tok = batch) and block tables of max_pages
+ * pages, on the current device.  Returns 0 and sets wc_last_error() on invalid
+ * arguments.  Zero-filled once after allocation; each call leaves it ready for
+ * the next one.  Calls sharing a workspace must be ordered on one stream.
+ */
+size_t wc_block_workspace_size(const wc_block_desc* desc, int32_t batch, int32_t n_tok, int32_t max_pages);
+
+/*
+ * Decode attention over a block-scaled cache, one query token per sequence:
+ *   out[b][hq][:] = sum_t p_t v^_t,  p = softmax_t(softmax_scale q . k^_t),  t < ctx_lens[b]
+ *   lse[b][hq]    = log sum_t e^(softmax_scale q . k^_t)
+ * fp32 sums and softmax statistics, out rounded once.  A sequence with no context gets out = 0 and
+ * lse = -inf.  What the pages hold past the context is never used.
+ *   q            [batch][Hq][128] act_type, rotated; q_stride elements from one token to the next
+ *   out          [batch][Hq][128] act_type; lse [batch][Hq] fp32 or NULL
+ *   k_scale, v_scale  NULL together: scale 1 (WC_CODE_E4M3 only)
+ *   softmax_scale     > 0, finite
+ *   workspace    >= wc_block_workspace_size(desc, batch, batch, max_pages) bytes, 256-byte
+ *                aligned; holds the device status word (wc_read_status): WC_DEV_BAD_PAGE (the page's
+ *                tokens are left out), _CTX (taken as no context), _TIMEOUT
+ */
+wc_status wc_block_decode_attention(const wc_block_desc* desc, int32_t act_type,
+                                    const void* q, int64_t q_stride,
+                                    const int32_t* block_table, int32_t max_pages,
+                                    const int32_t* ctx_lens, int32_t batch,
+                                    const void* k_codes, const void* v_codes,
+                                    const float* k_scale, const float* v_scale,
+                                    float softmax_scale, void* out, float* lse,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same attention for several query tokens per sequence (a prompt, a chunk of
+ * one, drafted tokens to verify): rows cu_q[b] .. cu_q[b + 1] - 1 of q are the last n_b
+ * tokens of sequence b's context, row i at position ctx_lens[b] - n_b + i.  causal != 0: a row
+ * attends to positions up to its own (one before the start attends to nothing:
+ * out = 0, lse = -inf); 0: to the whole context.
+ *   q            [n_tok][Hq][128]; out [n_tok][Hq][128]; lse [n_tok][Hq] or NULL (rows outside
+ *                every sequence's range are not written)
+ *   cu_q         [batch + 1] int32, ascending, cu_q[batch] <= n_tok
+ *   workspace    >= wc_block_workspace_size(desc, batch, n_tok, max_pages) bytes
+ */
+wc_status wc_block_extend_attention(const wc_block_desc* desc, int32_t act_type,
+                                    const void* q, int64_t q_stride, int32_t n_tok,
+                                    const int32_t* cu_q, const int32_t* block_table,
+                                    int32_t max_pages, const int32_t* ctx_lens, int32_t batch,
+                                    const void* k_codes, const void* v_codes,
+                                    const float* k_scale, const float* v_scale,
+                                    float softmax_scale, int32_t causal, void* out, float* lse,
+                                    void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Synchronises `stream`, copies the device status word held in `workspace`

@@ -13,9 +13,20 @@ fallback: importing this package without the compiled library raises.
     out, meter, meter_raw = wc.metered_decode_attention(desc, layer, q, block_table,
                                                         ctx_lens, cache, ws)
     keep_q, keep_kv, n_kept = wc.gate(meter_raw, group, tau)
+
+and for the unmetered 8-bit cache with one scale per page and head (rotation, append and
+attention, of one token or of many):
+
+    desc = wc.BlockDesc(num_q_heads=28, num_kv_heads=4, num_pages=n)
+    cache = wc.BlockCache.empty(desc, device="cuda")
+    q = wc.block_append(desc, k, v, ctx_lens, block_table, cache, cu_new=cu, cos=cos, sin=sin, q=q)
+    ws = wc.BlockWorkspace(desc, batch, n_tok, max_pages)
+    out = wc.block_extend_attention(desc, q, cu, block_table, ctx_lens, cache, ws)
+    out = wc.block_decode_attention(desc, q, block_table, ctx_lens, cache, ws)
 """
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -30,13 +41,19 @@ SCHEME_FP8_E4M3 = 1
 SCHEME_DITHER_INT8_G32 = 2
 ROPE_HALF = 0
 ROPE_INTERLEAVED = 1
+CODE_INT8 = 0
+CODE_E4M3 = 1
+ACT_FP16 = 0
+ACT_BF16 = 1
 DEV_BAD_SLOT, DEV_BAD_PAGE, DEV_BAD_CTX, DEV_TIMEOUT, DEV_BAD_PAIR, DEV_BAD_APPEND = 1, 2, 4, 8, 16, 32
+DEV_BAD_POSITION, DEV_BAD_ROWS = 64, 128
 EXPORTS = ("wc_kv_quantize_witness", "wc_workspace_size", "wc_metered_decode_attention",
            "wc_metered_decode_attention_tier_b", "wc_metered_decode_attention_noalloc",
            "wc_kv_quantize_witness_v", "wc_metered_decode_attention_v", "wc_gate_joint",
            "wc_metered_decode_attention_repair", "wc_repair_select",
            "wc_kv_quantize_witness_g32", "wc_metered_decode_attention_g32", "wc_select_bypass_pairs",
            "wc_metered_decode_attention_append", "wc_testing_decode_stalled_page",
+           "wc_block_append", "wc_block_workspace_size", "wc_block_decode_attention", "wc_block_extend_attention",
            "wc_gate", "wc_read_status", "wc_last_error", "wc_version")
 
 
@@ -90,6 +107,18 @@ def _load():
     lib.wc_metered_decode_attention_append.argtypes = [vp, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp,
                                                        vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.wc_metered_decode_attention_append.restype = ctypes.c_int
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    lib.wc_block_append.argtypes = [vp, i32, vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp, i32,
+                                    vp, vp, vp, vp, vp, vp]
+    lib.wc_block_append.restype = ctypes.c_int
+    lib.wc_block_workspace_size.argtypes = [vp, i32, i32, i32]
+    lib.wc_block_workspace_size.restype = ctypes.c_size_t
+    lib.wc_block_decode_attention.argtypes = [vp, i32, vp, i64, vp, i32, vp, i32, vp, vp, vp, vp, f32, vp, vp, vp,
+                                              ctypes.c_size_t, vp]
+    lib.wc_block_decode_attention.restype = ctypes.c_int
+    lib.wc_block_extend_attention.argtypes = [vp, i32, vp, i64, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp, f32, i32,
+                                              vp, vp, vp, ctypes.c_size_t, vp]
+    lib.wc_block_extend_attention.restype = ctypes.c_int
     lib.wc_read_status.argtypes = [vp, i32, vp, vp]
     lib.wc_read_status.restype = ctypes.c_int
     lib.wc_last_error.argtypes = []
@@ -437,9 +466,210 @@ def gate(meter_raw: torch.Tensor, group: int, tau: float, keep_q=None, keep_kv=N
     return keep_q, keep_kv, n_kept
 
 
+# ---- block-scaled 8-bit cache -------------------------------------------------------------------
+
+
+class _BlockDesc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("code", ctypes.c_int32),
+                ("rope_layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32)]
+
+
+@dataclass
+class BlockDesc:
+    """Mirror of ``wc_block_desc``."""
+    num_q_heads: int
+    num_kv_heads: int
+    num_pages: int
+    code: int = CODE_INT8
+    rope_layout: int = ROPE_HALF
+    rotary_dim: int = 128
+    head_dim: int = 128
+    page_size: int = 16
+
+    @property
+    def group(self):
+        return self.num_q_heads // self.num_kv_heads
+
+    def c(self):
+        return _BlockDesc(self.head_dim, self.num_q_heads, self.num_kv_heads, self.page_size, self.num_pages,
+                          self.code, self.rope_layout, self.rotary_dim)
+
+
+@dataclass
+class BlockCache:
+    """One layer's block-scaled cache tensors (layout in ``include/witcert.h``); without scales
+    (None) a cache of raw fp8 codes, such as a ``LayerCache``'s of the fp8 scheme."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_scale: Optional[torch.Tensor]
+    v_scale: Optional[torch.Tensor]
+
+    @staticmethod
+    def empty(desc: BlockDesc, device="cuda"):
+        shp = (desc.num_pages, desc.num_kv_heads)
+        codes = shp + (desc.page_size, desc.head_dim)
+        code_t = torch.uint8 if desc.code == CODE_E4M3 else torch.int8
+        return BlockCache(torch.zeros(codes, dtype=code_t, device=device), torch.zeros(codes, dtype=code_t, device=device),
+                          torch.zeros(shp, dtype=torch.float32, device=device),
+                          torch.zeros(shp, dtype=torch.float32, device=device))
+
+    def nbytes(self):
+        return sum(t.numel() * t.element_size() for t in (self.k_codes, self.v_codes, self.k_scale, self.v_scale)
+                   if t is not None)
+
+
+class BlockWorkspace:
+    """Zero-filled device workspace for the block attention calls of up to ``n_tok`` query tokens."""
+
+    def __init__(self, desc: BlockDesc, batch: int, n_tok: int, max_pages: int, device="cuda"):
+        d = desc.c()
+        self.nbytes = lib.wc_block_workspace_size(ctypes.byref(d), batch, n_tok, max_pages)
+        if self.nbytes == 0:
+            raise WitCertError(1, lib.wc_last_error().decode())
+        self.buf = torch.zeros(self.nbytes + 256, dtype=torch.uint8, device=device)
+        off = (-self.buf.data_ptr()) % 256
+        self.view = self.buf[off:off + self.nbytes]
+
+    def ptr(self):
+        return ctypes.c_void_p(self.view.data_ptr())
+
+
+_ACT = {torch.float16: ACT_FP16, torch.bfloat16: ACT_BF16}
+
+
+def _act(t: torch.Tensor):
+    a = _ACT.get(t.dtype)
+    if a is None:
+        raise ValueError(f"expected a float16 or bfloat16 tensor, got {t.dtype}")
+    return a
+
+
+def _rows(t: torch.Tensor, heads: int, act: int, name: str):
+    """Pointer and token stride of [n, heads, 128] rows whose heads are contiguous (a view of a
+    packed projection, for instance)."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != 128:
+        raise ValueError(f"{name} must be [n, {heads}, 128], got {list(shape)}")
+    if _ACT.get(t.dtype) != act:
+        raise ValueError(f"{name} has another element type: {t.dtype}")
+    s = t.stride()
+    if s[2] != 1 or (s[1] != 128 and heads > 1):
+        raise ValueError(f"{name}'s heads must be contiguous")
+    return t.data_ptr(), s[0] if shape[0] > 1 else max(s[0], heads * 128)
+
+
+def _ints(t: Optional[torch.Tensor], n: int, name: str):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() != n:
+        raise ValueError(f"{name} must hold {n} int32 values, got {t.numel()} {t.dtype}")
+    return _ptr(t)
+
+
+def _block_cache(desc: BlockDesc, cache: BlockCache):
+    n = desc.num_pages * desc.num_kv_heads
+    for t in (cache.k_codes, cache.v_codes):
+        if t.element_size() != 1 or t.numel() != n * desc.page_size * desc.head_dim:
+            raise ValueError("the cache's codes do not have the descriptor's shape")
+    for t in (cache.k_scale, cache.v_scale):
+        if t is not None and (t.dtype != torch.float32 or t.numel() != n):
+            raise ValueError("the cache's scales must be float32 [num_pages, num_kv_heads]")
+    return _ptr(cache.k_codes), _ptr(cache.v_codes), _ptr(cache.k_scale), _ptr(cache.v_scale)
+
+
+def block_append(desc: BlockDesc, k: torch.Tensor, v: torch.Tensor, ctx_lens: torch.Tensor, block_table: torch.Tensor,
+                 cache: BlockCache, cu_new: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+                 sin: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                 q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 dev_status: Optional[torch.Tensor] = None, stream=None):
+    """``wc_block_append``: k, v fp16 or bf16 [n_tok, Hkv, 128] (views with a token stride too), the last tokens of
+    contexts of ctx_lens int32 [B]; cu_new int32 [B + 1], None: one token per sequence; cos, sin fp32
+    [positions, rotary_dim / 2].  Returns the rotated queries (``q_out``) if ``q`` [n_tok, Hq, 128] is given."""
+    batch, max_pages = block_table.shape
+    act, n_tok = _act(k), k.shape[0]
+    kp, ks = _rows(k, desc.num_kv_heads, act, "k")
+    vp, vs = _rows(v, desc.num_kv_heads, act, "v")
+    if v.shape[0] != n_tok or (q is not None and q.shape[0] != n_tok):
+        raise ValueError("k, v and q must have the same number of tokens")
+    qp, qs = None, 0
+    if q is not None:
+        qp, qs = _rows(q, desc.num_q_heads, act, "q")
+        if q_out is None:
+            q_out = torch.empty(n_tok, desc.num_q_heads, 128, dtype=q.dtype, device=q.device)
+        elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+            raise ValueError("q_out must have q's shape and type")
+    num_positions = 0
+    if cos is not None:
+        num_positions = cos.shape[0]
+        for t in (cos, sin):
+            if t is None or t.dtype != torch.float32 or tuple(t.shape) != (num_positions, desc.rotary_dim // 2):
+                raise ValueError(f"cos and sin must be float32 [positions, {desc.rotary_dim // 2}]")
+    d = desc.c()
+    _check(lib.wc_block_append(
+        ctypes.byref(d), act, kp, ks, vp, vs, qp, qs, _ptr(q_out), n_tok, _ints(cu_new, batch + 1, "cu_new"),
+        _ints(block_table, batch * max_pages, "block_table"), max_pages, _ints(ctx_lens, batch, "ctx_lens"), batch,
+        _ints(positions, n_tok, "positions"), _ptr(cos), _ptr(sin), num_positions, *_block_cache(desc, cache),
+        _ptr(dev_status), _stream(stream)))
+    return q_out
+
+
+def _attention_out(desc, q, out, lse, return_lse):
+    n_tok = q.shape[0]
+    if out is None:
+        out = torch.empty(n_tok, desc.num_q_heads, 128, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's shape and type")
+    if lse is None:
+        lse = torch.empty(n_tok, desc.num_q_heads, dtype=torch.float32, device=q.device) if return_lse else None
+    elif lse.dtype != torch.float32 or lse.numel() != n_tok * desc.num_q_heads:
+        raise ValueError("lse must be float32 [n_tok, num_q_heads]")
+    return out, lse
+
+
+def block_decode_attention(desc: BlockDesc, q: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                           cache: BlockCache, ws: BlockWorkspace, softmax_scale: Optional[float] = None, out=None,
+                           lse=None, return_lse=False, stream=None):
+    """``wc_block_decode_attention``: q [B, Hq, 128], one token per sequence; softmax_scale 1 / sqrt(128) unless given.
+    Returns out, or (out, lse) with ``return_lse`` or an ``lse`` to fill."""
+    batch, max_pages = block_table.shape
+    act = _act(q)
+    qp, qs = _rows(q, desc.num_q_heads, act, "q")
+    if q.shape[0] != batch:
+        raise ValueError(f"q must have one token per sequence ({batch}), got {q.shape[0]}")
+    out, lse = _attention_out(desc, q, out, lse, return_lse)
+    d = desc.c()
+    _check(lib.wc_block_decode_attention(
+        ctypes.byref(d), act, qp, qs, _ints(block_table, batch * max_pages, "block_table"), max_pages,
+        _ints(ctx_lens, batch, "ctx_lens"), batch, *_block_cache(desc, cache),
+        1.0 / math.sqrt(128) if softmax_scale is None else softmax_scale, _ptr(out), _ptr(lse), ws.view.data_ptr(),
+        ws.nbytes, _stream(stream)))
+    return out if lse is None else (out, lse)
+
+
+def block_extend_attention(desc: BlockDesc, q: torch.Tensor, cu_q: torch.Tensor, block_table: torch.Tensor,
+                           ctx_lens: torch.Tensor, cache: BlockCache, ws: BlockWorkspace,
+                           softmax_scale: Optional[float] = None, causal=True, out=None, lse=None, return_lse=False,
+                           stream=None):
+    """``wc_block_extend_attention``: q [n_tok, Hq, 128], rows cu_q[b] .. cu_q[b + 1] - 1 the last tokens of sequence
+    b's context.  Returns out, or (out, lse) with ``return_lse`` or an ``lse`` to fill."""
+    batch, max_pages = block_table.shape
+    act = _act(q)
+    qp, qs = _rows(q, desc.num_q_heads, act, "q")
+    out, lse = _attention_out(desc, q, out, lse, return_lse)
+    d = desc.c()
+    _check(lib.wc_block_extend_attention(
+        ctypes.byref(d), act, qp, qs, q.shape[0], _ints(cu_q, batch + 1, "cu_q"),
+        _ints(block_table, batch * max_pages, "block_table"), max_pages, _ints(ctx_lens, batch, "ctx_lens"), batch,
+        *_block_cache(desc, cache), 1.0 / math.sqrt(128) if softmax_scale is None else softmax_scale, int(causal),
+        _ptr(out), _ptr(lse), ws.view.data_ptr(), ws.nbytes, _stream(stream)))
+    return out if lse is None else (out, lse)
+
+
 def read_status(ws_or_word, stream=None) -> int:
     """Synchronising read-and-clear of the device status word; returns the bits."""
-    if isinstance(ws_or_word, Workspace):
+    if isinstance(ws_or_word, (Workspace, BlockWorkspace)):
         p, is_word = ws_or_word.ptr(), 0
     else:
         p, is_word = _ptr(ws_or_word), 1

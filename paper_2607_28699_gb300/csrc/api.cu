@@ -6,13 +6,13 @@
 #include <mutex>
 #include <string>
 
+#include "api_checks.h"
 #include "wc_kernels.cuh"
 
-namespace {
+namespace wc {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
-wc_status fail(wc_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 wc_status fail(wc_status st, const char* fmt, ...) {
     char buf[512];
     va_list ap;
@@ -27,7 +27,21 @@ wc_status cuda_fail(cudaError_t e, const char* what) {
     return fail(WC_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+int current_sm_count(int* out) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return -1;
+    if (cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return -1;
+    return 0;
+}
+
+}  // namespace wc
+
+using wc::aligned16;
+using wc::cuda_fail;
+using wc::current_sm_count;
+using wc::fail;
+
+namespace {
 
 // allow_grouped: the grouped scheme is accepted only by its own (_g32) entry
 // points and the workspace query; every other entry point rejects it.
@@ -76,20 +90,13 @@ wc_status check_cache(const wc_cache_desc* d, const void* kc, const void* vc, co
     return WC_OK;
 }
 
-int current_sm_count(int* out) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return -1;
-    if (cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return -1;
-    return 0;
-}
-
 }  // namespace
 
 extern "C" {
 
 int32_t wc_version(void) { return (1 << 16) | 0; }
 
-const char* wc_last_error(void) { return g_last_error.c_str(); }
+const char* wc_last_error(void) { return wc::g_last_error.c_str(); }
 
 // Bypass arguments of the grouped scheme: m in [0, 16]; the pair list and the
 // exact-value array are required when m > 0.

@@ -1,0 +1,100 @@
+// The block-scaled 8-bit cache: launch parameters and device helpers of its kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "wc_kernels.cuh"
+
+namespace wc {
+
+struct BlockAppendParams {
+    const void* x[2];          // new keys and values, rows of x_stride elements per token
+    int64_t x_stride[2];
+    const void* q;             // queries to rotate, nullptr: none
+    int64_t q_stride;
+    void* q_out;
+    const int32_t* cu_new;     // nullptr: one token per sequence
+    const int32_t* block_table;
+    const int32_t* ctx_lens;
+    const int32_t* positions;  // nullptr: the logical positions
+    const float* cos_table;
+    const float* sin_table;
+    uint8_t* codes[2];
+    float* scale[2];
+    uint32_t* dev_status;      // optional
+    int32_t n_tok, batch, max_pages, num_pages, num_q_heads, num_kv_heads, num_positions, rotary_dim;
+    int32_t page_tasks;        // upper bound of the pages written, over all sequences
+    int32_t page_ctas;         // CTAs of the page tasks; those after them rotate queries
+};
+
+struct BlockAttentionParams {
+    const void* q;
+    int64_t q_stride;
+    const int32_t* cu_q;       // nullptr: one token per sequence
+    const int32_t* block_table;
+    const int32_t* ctx_lens;
+    const uint8_t* codes[2];
+    const float* scale[2];     // nullptr: 1
+    void* out;
+    float* lse;                // optional
+    uint32_t* status;
+    float* partials;
+    float scale_log2;          // softmax_scale * log2(e)
+    int32_t n_tok, batch, max_pages, num_pages, num_q_heads, num_kv_heads, group, causal;
+    int32_t bf16;              // element type of q and out
+};
+
+cudaError_t launch_block_append(const BlockAppendParams& p, int code, int act, int rope_layout, cudaStream_t stream);
+cudaError_t launch_block_attention_simple(const BlockAttentionParams& p, int code, cudaStream_t stream);
+
+// ---- device helpers ---------------------------------------------------------------------------
+
+__device__ __forceinline__ float2 h2_to_float2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+
+// Two elements of act_type (fp16 or bf16) as fp32: exact.
+template <bool kBf16>
+__device__ __forceinline__ float2 act2_to_float2(uint32_t w) {
+    if constexpr (kBf16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    else return h2_to_float2(w);
+}
+
+template <bool kBf16>
+__device__ __forceinline__ uint32_t float2_to_act2(float lo, float hi) {
+    if constexpr (kBf16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        return pack_h2(lo, hi);
+    }
+}
+
+// Four codes of a word as two exact half2 (codes 0, 1 and 2, 3).
+template <int kCode>
+__device__ __forceinline__ void codes4_to_h2(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if constexpr (kCode == WC_CODE_INT8) {
+        const uint32_t x = w ^ 0x80808080u;
+        lo = s8x2_to_h2(x, 0x4140u);
+        hi = s8x2_to_h2(x, 0x4342u);
+    } else {
+        lo = e4m3x2_to_h2(w);
+        hi = e4m3x2_to_h2(w >> 16);
+    }
+}
+
+// The sequence whose first[b] is the last one <= x, for ascending first(0) <= x; a warp searches together.
+template <typename F>
+__device__ __forceinline__ int warp_find_last(int n, long long x, F first) {
+    int lo = 0;
+    for (int len = n; len > 1;) {
+        const int step = (len + 31) / 32;
+        const int at = lo + (threadIdx.x & 31) * step;
+        const bool le = at < lo + len && first(at) <= x;
+        const int k = __popc(__ballot_sync(0xffffffffu, le)) - 1;   // lane 0 holds by assumption
+        const int next = lo + max(k, 0) * step;
+        len = min(step, lo + len - next);
+        lo = next;
+    }
+    return lo;
+}
+
+}  // namespace wc
