@@ -26,13 +26,19 @@ wc_status check_block_desc(const wc_block_desc* d) {
         return fail(WC_ERR_UNSUPPORTED, "num_q_heads / num_kv_heads must be at most %d (got %d)", kMaxBlockGroup,
                     d->num_q_heads / d->num_kv_heads);
     if (d->num_pages < 1) return fail(WC_ERR_INVALID_ARG, "num_pages must be positive (got %d)", d->num_pages);
-    if ((long long)d->num_pages * wc::kPage > 0x7FFFFFFFLL)
-        return fail(WC_ERR_UNSUPPORTED, "num_pages * 16 must fit in int32");
+    if ((long long)d->num_pages * wc::kPage > 0x7FFFFFFFLL || (long long)d->num_pages * d->num_kv_heads > 0x7FFFFFFFLL)
+        return fail(WC_ERR_UNSUPPORTED, "num_pages * 16 and num_pages * num_kv_heads must fit in int32");
     if (d->code != WC_CODE_INT8 && d->code != WC_CODE_E4M3) return fail(WC_ERR_UNSUPPORTED, "unknown code %d", d->code);
     if (d->rope_layout != WC_ROPE_HALF && d->rope_layout != WC_ROPE_INTERLEAVED)
         return fail(WC_ERR_UNSUPPORTED, "unknown rope_layout %d", d->rope_layout);
     if (d->rotary_dim < 0 || d->rotary_dim > wc::kHeadDim || d->rotary_dim % 16 != 0)
         return fail(WC_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16 up to 128 (got %d)", d->rotary_dim);
+    return WC_OK;
+}
+
+wc_status check_positions(const wc_block_desc* d, int32_t max_pages) {
+    if ((long long)max_pages * d->num_kv_heads > 0x7FFFFFFFLL)
+        return fail(WC_ERR_UNSUPPORTED, "max_pages * num_kv_heads must fit in int32");
     return WC_OK;
 }
 
@@ -63,9 +69,11 @@ wc_status check_block_cache(const void* kc, const void* vc, const float* ks, con
     return WC_OK;
 }
 
-size_t workspace_bytes_for(const wc_block_desc* desc, int32_t batch, int32_t n_tok, int32_t max_pages) {
-    (void)desc, (void)batch, (void)n_tok, (void)max_pages;
-    return 256;
+size_t workspace_bytes_for(const wc_block_desc* desc, int32_t batch, int32_t n_tok, int32_t max_pages, int num_sms) {
+    (void)n_tok;
+    const int group = desc->num_q_heads / desc->num_kv_heads;
+    if (group > wc::kMaxGroup) return 256;
+    return (256 + wc::block_decode_workspace(batch, desc->num_kv_heads, group, max_pages, num_sms) + 255) & ~(size_t)255;
 }
 
 wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, int64_t q_stride, int32_t n_tok,
@@ -75,6 +83,7 @@ wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, 
                     void* stream) {
     if (wc_status st = check_block_desc(desc)) return st;
     if (wc_status st = check_sizes(act_type, batch, n_tok, max_pages)) return st;
+    if (wc_status st = check_positions(desc, max_pages)) return st;
     if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale))
         return fail(WC_ERR_INVALID_ARG, "softmax_scale must be positive and finite (got %g)", (double)softmax_scale);
     if (!k_scale != !v_scale) return fail(WC_ERR_INVALID_ARG, "k_scale and v_scale are NULL together or not at all");
@@ -88,7 +97,9 @@ wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, 
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
         return fail(WC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     if (wc_status st = check_block_cache(k_codes, v_codes, k_scale, v_scale)) return st;
-    const size_t need = workspace_bytes_for(desc, batch, n_tok, max_pages);
+    int sms = 0;
+    if (wc::current_sm_count(&sms) != 0) return fail(WC_ERR_CUDA, "cannot query the current device");
+    const size_t need = workspace_bytes_for(desc, batch, n_tok, max_pages, sms);
     if (workspace_bytes < need) return fail(WC_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
     wc::BlockAttentionParams p = {};
     p.q = q;
@@ -114,7 +125,9 @@ wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, 
     p.group = desc->num_q_heads / desc->num_kv_heads;
     p.causal = causal != 0;
     p.bf16 = act_type == WC_ACT_BF16;
-    const cudaError_t e = wc::launch_block_attention_simple(p, desc->code, static_cast<cudaStream_t>(stream));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = !ragged && p.group <= wc::kMaxGroup ? wc::launch_block_decode(p, desc->code, sms, s)
+                                                               : wc::launch_block_attention_simple(p, desc->code, s);
     return e == cudaSuccess ? WC_OK : cuda_fail(e, "block attention kernel launch");
 }
 
@@ -182,12 +195,19 @@ wc_status wc_block_append(const wc_block_desc* desc, int32_t act_type, const voi
 }
 
 size_t wc_block_workspace_size(const wc_block_desc* desc, int32_t batch, int32_t n_tok, int32_t max_pages) {
-    if (check_block_desc(desc) != WC_OK || check_sizes(WC_ACT_FP16, batch, n_tok, max_pages) != WC_OK) return 0;
+    if (check_block_desc(desc) != WC_OK || check_sizes(WC_ACT_FP16, batch, n_tok, max_pages) != WC_OK ||
+        check_positions(desc, max_pages) != WC_OK)
+        return 0;
     if (batch < 1 || n_tok < 1) {
         fail(WC_ERR_INVALID_ARG, "batch and n_tok must be positive");
         return 0;
     }
-    return workspace_bytes_for(desc, batch, n_tok, max_pages);
+    int sms = 0;
+    if (wc::current_sm_count(&sms) != 0) {
+        fail(WC_ERR_CUDA, "no current CUDA device to size the workspace for");
+        return 0;
+    }
+    return workspace_bytes_for(desc, batch, n_tok, max_pages, sms);
 }
 
 wc_status wc_block_decode_attention(const wc_block_desc* desc, int32_t act_type, const void* q, int64_t q_stride,

@@ -3,6 +3,8 @@
 
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "wc_kernels.cuh"
 
 namespace wc {
@@ -45,6 +47,10 @@ struct BlockAttentionParams {
 };
 
 cudaError_t launch_block_append(const BlockAppendParams& p, int code, int act, int rope_layout, cudaStream_t stream);
+// Sequences of one launch of the decode: their page counts' sums sit in shared memory.
+constexpr int kDecodeBatch = 2048;
+size_t block_decode_workspace(int batch, int num_kv_heads, int group, int max_pages, int num_sms);
+cudaError_t launch_block_decode(const BlockAttentionParams& p, int code, int num_sms, cudaStream_t stream);   // group <= kMaxGroup
 cudaError_t launch_block_attention_simple(const BlockAttentionParams& p, int code, cudaStream_t stream);
 
 // ---- device helpers ---------------------------------------------------------------------------
@@ -79,6 +85,46 @@ __device__ __forceinline__ void codes4_to_h2(uint32_t w, uint32_t& lo, uint32_t&
         lo = e4m3x2_to_h2(w);
         hi = e4m3x2_to_h2(w >> 16);
     }
+}
+
+__device__ __forceinline__ uint16_t float_to_act(float x, bool bf16) {
+    return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+}
+
+// log(sum of 2^m l), -inf for an empty sum.
+__device__ __forceinline__ float log_sum(float m, float l) {
+    return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// A warp's output row: four channels a lane, divided by the sum of weights.
+__device__ __forceinline__ void store_output(const BlockAttentionParams& p, size_t cell, int lane, float4 o, float m, float l) {
+    const float f = l == 0.0f ? 0.0f : __frcp_rn(l);
+    const uint32_t lo = p.bf16 ? float2_to_act2<true>(o.x * f, o.y * f) : pack_h2(o.x * f, o.y * f);
+    const uint32_t hi = p.bf16 ? float2_to_act2<true>(o.z * f, o.w * f) : pack_h2(o.z * f, o.w * f);
+    reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + cell * kHeadDim)[lane] = make_uint2(lo, hi);
+    if (p.lse && lane == 0) p.lse[cell] = log_sum(m, l);
+}
+
+// N words of bf16 pairs of one row (the rest held by other lanes: across takes the maximum over
+// them) to fp16 pairs times a power of two that puts the row's largest value below 2^15: all of bf16's
+// bits stay but those below 2^-39 of the largest.  Returns the inverse factor.  Rows of zeros, infinities and NaN
+// are converted as they are.
+template <int N, typename F>
+__device__ __forceinline__ float bf16_row_to_f16(uint32_t (&w)[N], F across) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, max(w[i] << 16 & 0x7FFFFFFFu, w[i] & 0x7FFF0000u));
+    top = across(top);
+    int e = (int)(top >> 23) - 127;   // the largest is below 2^(e + 1)
+    if (top == 0 || e == 128) e = 14;
+    const int shift = max(min(14 - e, 126), -126);
+    const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float2 f = act2_to_float2<true>(w[i]);
+        w[i] = pack_h2(f.x * up, f.y * up);
+    }
+    return __uint_as_float((uint32_t)(127 - shift) << 23);
 }
 
 // The sequence whose first[b] is the last one <= x, for ascending first(0) <= x; a warp searches together.
