@@ -16,8 +16,8 @@ OUT_DIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(OUT_DIR, "libwitcert.so")
 LIB_METER_OFF = os.path.join(OUT_DIR, "libwitcert_meteroff.so")
 SOURCES = ["api.cu", "write_kernel.cu", "decode_kernel.cu", "gate_kernel.cu", "repair_kernel.cu",
-           "decode_g32_kernel.cu", "block_api.cu", "block_append_kernel.cu", "block_simple_kernel.cu",
-           "block_decode_kernel.cu"]
+           "decode_g32_kernel.cu", "block_api.cu", "block_append_kernel.cu",
+           "block_decode_kernel.cu", "block_extend_kernel.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]
 

@@ -36,9 +36,11 @@ wc_status check_block_desc(const wc_block_desc* d) {
     return WC_OK;
 }
 
-wc_status check_positions(const wc_block_desc* d, int32_t max_pages) {
+wc_status check_positions(const wc_block_desc* d, int32_t n_tok, int32_t max_pages) {
     if ((long long)max_pages * d->num_kv_heads > 0x7FFFFFFFLL)
         return fail(WC_ERR_UNSUPPORTED, "max_pages * num_kv_heads must fit in int32");
+    if ((long long)n_tok * d->num_q_heads > 0x7FFFFFFFLL)
+        return fail(WC_ERR_UNSUPPORTED, "n_tok * num_q_heads must fit in int32");
     return WC_OK;
 }
 
@@ -69,11 +71,12 @@ wc_status check_block_cache(const void* kc, const void* vc, const float* ks, con
     return WC_OK;
 }
 
-size_t workspace_bytes_for(const wc_block_desc* desc, int32_t batch, int32_t n_tok, int32_t max_pages, int num_sms) {
-    (void)n_tok;
+// The same for fewer sequences, tokens and pages or less.
+size_t workspace_bytes_for(const wc_block_desc* desc, int32_t n_tok, int num_sms) {
     const int group = desc->num_q_heads / desc->num_kv_heads;
-    if (group > wc::kMaxGroup) return 256;
-    return (256 + wc::block_decode_workspace(batch, desc->num_kv_heads, group, max_pages, num_sms) + 255) & ~(size_t)255;
+    const size_t decode = group <= wc::kMaxGroup ? wc::block_decode_workspace(group, num_sms) : 0;
+    const size_t extend = wc::block_extend_workspace(n_tok, desc->num_q_heads, num_sms);
+    return (256 + wc::block_arrived_bytes(num_sms) + std::max(decode, extend) + 255) & ~(size_t)255;
 }
 
 wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, int64_t q_stride, int32_t n_tok,
@@ -83,7 +86,7 @@ wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, 
                     void* stream) {
     if (wc_status st = check_block_desc(desc)) return st;
     if (wc_status st = check_sizes(act_type, batch, n_tok, max_pages)) return st;
-    if (wc_status st = check_positions(desc, max_pages)) return st;
+    if (wc_status st = check_positions(desc, n_tok, max_pages)) return st;
     if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale))
         return fail(WC_ERR_INVALID_ARG, "softmax_scale must be positive and finite (got %g)", (double)softmax_scale);
     if (!k_scale != !v_scale) return fail(WC_ERR_INVALID_ARG, "k_scale and v_scale are NULL together or not at all");
@@ -99,7 +102,7 @@ wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, 
     if (wc_status st = check_block_cache(k_codes, v_codes, k_scale, v_scale)) return st;
     int sms = 0;
     if (wc::current_sm_count(&sms) != 0) return fail(WC_ERR_CUDA, "cannot query the current device");
-    const size_t need = workspace_bytes_for(desc, batch, n_tok, max_pages, sms);
+    const size_t need = workspace_bytes_for(desc, n_tok, sms);
     if (workspace_bytes < need) return fail(WC_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
     wc::BlockAttentionParams p = {};
     p.q = q;
@@ -127,7 +130,7 @@ wc_status attention(const wc_block_desc* desc, int32_t act_type, const void* q, 
     p.bf16 = act_type == WC_ACT_BF16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = !ragged && p.group <= wc::kMaxGroup ? wc::launch_block_decode(p, desc->code, sms, s)
-                                                               : wc::launch_block_attention_simple(p, desc->code, s);
+                                                               : wc::launch_block_extend(p, desc->code, sms, s);
     return e == cudaSuccess ? WC_OK : cuda_fail(e, "block attention kernel launch");
 }
 
@@ -196,7 +199,7 @@ wc_status wc_block_append(const wc_block_desc* desc, int32_t act_type, const voi
 
 size_t wc_block_workspace_size(const wc_block_desc* desc, int32_t batch, int32_t n_tok, int32_t max_pages) {
     if (check_block_desc(desc) != WC_OK || check_sizes(WC_ACT_FP16, batch, n_tok, max_pages) != WC_OK ||
-        check_positions(desc, max_pages) != WC_OK)
+        check_positions(desc, n_tok, max_pages) != WC_OK)
         return 0;
     if (batch < 1 || n_tok < 1) {
         fail(WC_ERR_INVALID_ARG, "batch and n_tok must be positive");
@@ -207,7 +210,7 @@ size_t wc_block_workspace_size(const wc_block_desc* desc, int32_t batch, int32_t
         fail(WC_ERR_CUDA, "no current CUDA device to size the workspace for");
         return 0;
     }
-    return workspace_bytes_for(desc, batch, n_tok, max_pages, sms);
+    return workspace_bytes_for(desc, n_tok, sms);
 }
 
 wc_status wc_block_decode_attention(const wc_block_desc* desc, int32_t act_type, const void* q, int64_t q_stride,

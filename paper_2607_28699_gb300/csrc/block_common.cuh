@@ -49,9 +49,13 @@ struct BlockAttentionParams {
 cudaError_t launch_block_append(const BlockAppendParams& p, int code, int act, int rope_layout, cudaStream_t stream);
 // Sequences of one launch of the decode: their page counts' sums sit in shared memory.
 constexpr int kDecodeBatch = 2048;
-size_t block_decode_workspace(int batch, int num_kv_heads, int group, int max_pages, int num_sms);
+// A workspace: status word (256 bytes), the decode's arrival counts (a place of their own: they are 0 between
+// calls), then what either kernel needs.
+inline size_t block_arrived_bytes(int num_sms) { return ((size_t)num_sms * sizeof(int) + 255) & ~(size_t)255; }
+size_t block_decode_workspace(int group, int num_sms);
 cudaError_t launch_block_decode(const BlockAttentionParams& p, int code, int num_sms, cudaStream_t stream);   // group <= kMaxGroup
-cudaError_t launch_block_attention_simple(const BlockAttentionParams& p, int code, cudaStream_t stream);
+size_t block_extend_workspace(int n_tok, int num_q_heads, int num_sms);
+cudaError_t launch_block_extend(const BlockAttentionParams& p, int code, int num_sms, cudaStream_t stream);
 
 // ---- device helpers ---------------------------------------------------------------------------
 

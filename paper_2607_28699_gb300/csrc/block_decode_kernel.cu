@@ -25,7 +25,7 @@ constexpr int kStages = 3;
 constexpr int kPageBytes = kPage * kHeadDim;           // one head's page of keys, or of values
 constexpr int kStageBytes = 2 * kPageBytes;
 constexpr int kRow = kHeadDim + 4;                     // floats of a merge row in shared memory
-constexpr int kMinPages = 2;                           // per warp, before a launch takes more CTAs
+constexpr int kMinPages = 1;                           // per warp, before a launch takes more CTAs
 constexpr float kNoMax = -1e30f;                       // the running maximum before the first logit
 constexpr float kSlack = 8.0f;                         // log2 units a logit may pass it by
 
@@ -35,15 +35,24 @@ struct DecodeArgs {
     // Of the unit that begins in CTA c and reaches past it: CTAs that left a partial result; 0 between
     // calls.  Its place does not depend on a call's sizes.
     int* arrived;
-    float* partials;        // [grid][2 + kWarps] slots: of the CTA's first and last unit, of a warp's first
+    int by_head;             // the shares are of one head's pages
+    float* partials;         // [grid][2 + kWarps] slots: of the CTA's first and last unit, of a warp's first
 };
+
+// A unit (head, sequence), its pages' positions and the CTAs that read them.
+struct Unit {
+    int id, start, end, c0, c1;
+};
+constexpr int kSequenceBits = 11;
+static_assert(kDecodeBatch <= 1 << kSequenceBits);   // id: head << kSequenceBits | sequence
 
 struct Shared {
     int prefix[kDecodeBatch + 1];   // pages of one head before each sequence
     int ctx[kDecodeBatch];
     int warp_sum[kWarps];
     int entry[2 * kWarps];   // units of the warps' unfinished results (a warp's first, its last), -1: none
-    int open[2];             // units of the CTA's two slots, -1: none; then: merged here
+    Unit ends[2];            // the units of the CTA's first and last page
+    int open[2];             // slot 0, 1 holds a partial result of ends[0], ends[1]; then: to be merged here
     uint64_t bars[kWarps][kStages];
 };
 constexpr int kRingBytes = kWarps * kStages * kStageBytes;
@@ -54,6 +63,8 @@ static_assert(kMaxGroup * kRow * 4 <= kStages * kStageBytes, "a warp's last resu
 __host__ __device__ __forceinline__ size_t slot_floats(int group) { return ((size_t)group * (kHeadDim + 2) + 3) & ~(size_t)3; }
 
 // How [0, total) is cut: the first `more` CTAs take len + 1 pages, the others len; total < 2^31.
+// Where the grid is a multiple of the heads, or one sequence is all there is, each head's pages are
+// cut by themselves (no CTA then reads two units of one sequence), else all heads' laid end to end.
 struct Shares {
     int used, len, more;
     __device__ __forceinline__ Shares(int total, int grid) {
@@ -128,20 +139,20 @@ __device__ __forceinline__ int sequence_at(const Shared& s, int batch, int r) {
 // What a lane knows of one page of its warp's range.
 struct PageEntry {
     int row;       // first row of the code arrays' (page, head) index
-    int unit;      // head * batch + sequence
+    int unit;      // Unit::id
     int info;      // tokens to read | kFirst | kLast
     float ks, vs;  // key scale, value scale
 };
 constexpr int kTokens = 31, kFirst = 32, kLast = 64;
 
-__device__ __forceinline__ PageEntry page_entry(const BlockAttentionParams& p, const Shared& s, int per_head, int at, int first, int last) {
+__device__ __forceinline__ PageEntry page_entry(const BlockAttentionParams& p, const Shared& s, int head0, int per_head, int at, int first, int last) {
     PageEntry e = {0, 0, 0, 0.0f, 1.0f};
     if (at >= last) return e;
-    const int head = (unsigned)at / (unsigned)per_head, r = at - head * per_head;
+    const int k = at < per_head ? 0 : (int)((unsigned)at / (unsigned)per_head), head = head0 + k, r = at - k * per_head;
     const int b = sequence_at(s, p.batch, r), page = r - s.prefix[b];
     const int phys = load_dep(p.block_table + (size_t)b * p.max_pages + page);
     int tokens = min(kPage, s.ctx[b] - page * kPage);
-    e.unit = head * p.batch + b;
+    e.unit = head << kSequenceBits | b;
     e.info = (page == 0 || at == first ? kFirst : 0) | (page + 1 == s.prefix[b + 1] - s.prefix[b] || at + 1 == last ? kLast : 0);
     if (phys < 0 || phys >= p.num_pages) {
         atomicOr(p.status, WC_DEV_BAD_PAGE);
@@ -220,7 +231,6 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
     grid_dep_launch();
     page_prefix(p, s, blockIdx.x == 0);
     const int per_head = s.prefix[p.batch];
-    const int total = per_head * p.num_kv_heads;
     // sequences without context: nothing to add up
     for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
         if (s.prefix[b + 1] > s.prefix[b]) continue;
@@ -228,19 +238,22 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
             static_cast<uint32_t*>(p.out)[(size_t)b * p.num_q_heads * (kHeadDim / 2) + i] = 0;
         for (int i = threadIdx.x; p.lse && i < p.num_q_heads; i += kThreads) p.lse[(size_t)b * p.num_q_heads + i] = -INFINITY;
     }
-    if (total == 0) return;
-    const Shares shares(total, gridDim.x);
-    const int cta = blockIdx.x;
+    if (per_head == 0) return;
+    const bool by_head = args.by_head;
+    const int heads = by_head ? 1 : p.num_kv_heads, per_part = by_head ? gridDim.x / p.num_kv_heads : gridDim.x;
+    const int part0 = by_head ? blockIdx.x / per_part : 0, cta0 = part0 * per_part, head0 = part0;   // this part's first CTA and head
+    const Shares shares(per_head * heads, per_part);
+    const int cta = blockIdx.x - cta0;
     if (cta >= shares.used) return;
     const int a = shares.begin(cta), e = shares.begin(cta + 1);
     const int first = warp_begin(a, e, warp), last = warp_begin(a, e, warp + 1), n = last - first;
-    float* cta_slots = args.partials + (size_t)cta * (2 + kWarps) * slot_floats(p.group);
+    float* cta_slots = args.partials + (size_t)blockIdx.x * (2 + kWarps) * slot_floats(p.group);
     if (lane < 2) s.entry[2 * warp + lane] = -1;   // read after the CTA's next barrier
-    if (threadIdx.x < 2) s.open[threadIdx.x] = -1;
+    if (threadIdx.x < 2) s.open[threadIdx.x] = 0;
     __syncwarp();
     uint8_t* stage0 = ring + warp * kStages * kStageBytes;
-    PageEntry cur = page_entry(p, s, per_head, first + lane, first, last), next = {};
-    if (n > 32) next = page_entry(p, s, per_head, first + 32 + lane, first, last);
+    PageEntry cur = page_entry(p, s, head0, per_head, first + lane, first, last), next = {};
+    if (n > 32) next = page_entry(p, s, head0, per_head, first + 32 + lane, first, last);
     int issued = 0;
     auto issue = [&](int i, int row) {   // page i of the warp's range
         issued = i + 1;
@@ -257,6 +270,15 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         const int row = __shfl_sync(0xffffffffu, cur.row, i);
         if (i < n) issue(i, row);
     }
+    if (warp == kWarps - 1 && lane < 2) {   // while the first pages come
+        const int at = lane ? e - 1 : a, k = at < per_head ? 0 : (int)((unsigned)at / (unsigned)per_head);
+        const int b = sequence_at(s, p.batch, at - k * per_head);
+        Unit u = {(head0 + k) << kSequenceBits | b, k * per_head + s.prefix[b], k * per_head + s.prefix[b + 1], 0, 0};
+        u.c0 = shares.cta_at(u.start);
+        u.c1 = shares.cta_at(u.end - 1);
+        s.ends[lane] = u;
+    }
+    __syncwarp();
 
     uint32_t q[16];
     float acc[8][4];
@@ -273,8 +295,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         const bool no_values = vs == 0.0f;   // the codes count as 0 then, whatever they are
         if (no_values) vs = 1.0f;
         if (info & kFirst) {
-            const int unit = __shfl_sync(0xffffffffu, cur.unit, from), head = unit / p.batch;
-            const float f = load_queries(p, unit - head * p.batch, head, q);
+            const int unit = __shfl_sync(0xffffffffu, cur.unit, from);
+            const float f = load_queries(p, unit & ((1 << kSequenceBits) - 1), unit >> kSequenceBits, q);
             qf[0] = __shfl_sync(0xffffffffu, f, 8 * t);       // of head 2 t
             qf[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);   // of head 2 t + 1
 #pragma unroll
@@ -366,8 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], o);
-            const int unit = __shfl_sync(0xffffffffu, cur.unit, from), head = unit / p.batch, b = unit - head * p.batch;
-            const int start = head * per_head + s.prefix[b], end = head * per_head + s.prefix[b + 1];
+            const int unit = __shfl_sync(0xffffffffu, cur.unit, from), head = unit >> kSequenceBits, b = unit & ((1 << kSequenceBits) - 1);
+            const int start = (head - head0) * per_head + s.prefix[b], end = (head - head0) * per_head + s.prefix[b + 1];
             const bool whole = start == seg && end == first + i + 1, final = i == n - 1;
             if (whole) {
 #pragma unroll
@@ -407,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         }
         if (from == 31) {
             cur = next;
-            if (i + 33 < n) next = page_entry(p, s, per_head, first + i + 33 + lane, first, last);
+            if (i + 33 < n) next = page_entry(p, s, head0, per_head, first + i + 33 + lane, first, last);
         }
     }
     if (!ok) {   // copies still in flight end before the CTA does (bounded again)
@@ -418,14 +440,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
 
     // the CTA's unfinished results (lane k looks after entry k; those of one unit follow each other), a query
     // head per warp
-    auto start_of = [&](int unit) { return (int)((unsigned)unit / p.batch) * per_head + s.prefix[(unsigned)unit % p.batch]; };
-    auto end_of = [&](int unit) { return (int)((unsigned)unit / p.batch) * per_head + s.prefix[(unsigned)unit % p.batch + 1]; };
     auto finish = [&](int unit, int hq, float4 o, float m, float l) {
-        const int head = (unsigned)unit / p.batch, b = unit - head * p.batch;
+        const int head = unit >> kSequenceBits, b = unit & ((1 << kSequenceBits) - 1);
         store_output(p, (size_t)b * p.num_q_heads + head * p.group + hq, lane, o, m, l);
     };
     if (warp < p.group) {
-        const int mine = s.entry[lane];
+        const int mine = lane < 2 * kWarps ? s.entry[lane] : -1;
         const float* rows = reinterpret_cast<const float*>(ring) + warp * kRow;   // of the warps' last results
         constexpr int kPitch = kStages * kStageBytes / 4;
         for (uint32_t left = __ballot_sync(0xffffffffu, mine >= 0); left;) {
@@ -439,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                               : *reinterpret_cast<const float2*>(cta_slots + (2 + (lane >> 1)) * slot_floats(p.group) + p.group * kHeadDim + 2 * warp);
             const float top = warp_max(ml.x), f = fast_exp2(ml.x - top), sum = warp_sum(f * ml.y);
             float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (members == 0xAAAAAAAAu) {
+            if (members == (0xAAAAAAAAu >> (32 - 2 * kWarps))) {
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w)
                     fma4(o, __shfl_sync(0xffffffffu, f, 2 * w + 1), *reinterpret_cast<const float4*>(rows + w * kPitch + 4 * lane));
@@ -450,57 +470,69 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                     fma4(o, __shfl_sync(0xffffffffu, f, k), *reinterpret_cast<const float4*>(x + 4 * lane));
                 }
             }
-            const int start = start_of(unit);
-            if (start >= a && end_of(unit) <= e) {
+            const bool before = unit == s.ends[0].id && s.ends[0].start < a, after = unit == s.ends[1].id && s.ends[1].end > e;
+            if (!before && !after) {
                 finish(unit, warp, o, top, sum);
                 continue;
             }
-            const int which = start < a ? 0 : 1;
+            const int which = before ? 0 : 1;
             float* slot = cta_slots + which * slot_floats(p.group);
             *reinterpret_cast<float4*>(slot + warp * kHeadDim + 4 * lane) = o;
             if (lane == 0) {
                 *reinterpret_cast<float2*>(slot + p.group * kHeadDim + 2 * warp) = make_float2(top, sum);
-                if (warp == 0) s.open[which] = unit;
+                if (warp == 0) s.open[which] = 1;
             }
         }
     }
     __syncthreads();
-    if (threadIdx.x < 2 && s.open[threadIdx.x] >= 0) {
-        const int unit = s.open[threadIdx.x];
-        const int c0 = shares.cta_at(start_of(unit)), ctas = shares.cta_at(end_of(unit) - 1) - c0 + 1;
-        if (add_acq_rel(args.arrived + c0, 1) == ctas - 1) args.arrived[c0] = 0;
-        else s.open[threadIdx.x] = -1;
+    if (threadIdx.x < 2 && s.open[threadIdx.x]) {
+        const Unit& u = s.ends[threadIdx.x];
+        int* arrived = args.arrived + cta0 + u.c0;
+        if (add_acq_rel(arrived, 1) == u.c1 - u.c0) *arrived = 0;
+        else s.open[threadIdx.x] = 0;
     }
     __syncthreads();
     float* rows = reinterpret_cast<float*>(ring);
     const int parts = kWarps / p.group, part = warp / p.group, hq = warp - part * p.group;   // warps per query head
     for (int which = 0; which < 2; ++which) {
-        const int unit = s.open[which];
-        if (unit < 0) continue;
-        const int c0 = shares.cta_at(start_of(unit)), c1 = shares.cta_at(end_of(unit) - 1);
+        if (!s.open[which]) continue;
+        const int unit = s.ends[which].id, c0 = cta0 + s.ends[which].c0, c1 = cta0 + s.ends[which].c1;
         float m = kNoMax, l = 0.0f;
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (part < parts) {
             // CTA c0 left its result in its second slot, the others in their first
-            auto slot_of = [&](int c) { return args.partials + ((size_t)c * (2 + kWarps) + (c == c0)) * slot_floats(p.group); };
-            for (int c = c0 + part; c <= c1; c += 32 * parts) {
-                const int mine = c + lane * parts;
+            const int slot = (int)slot_floats(p.group), pitch = (2 + kWarps) * slot, ml_at = p.group * kHeadDim + 2 * hq, o_at = hq * kHeadDim + 4 * lane;
+            const float* base = args.partials + c0 * pitch;
+            if (part == 0) {
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(base + slot + ml_at));
+                o = __ldcg(reinterpret_cast<const float4*>(base + slot + o_at));
+                m = ml.x;
+                l = ml.y;
+            }
+            base += (1 + part) * pitch;
+            const int step = parts * pitch, mine = c1 - c0 > part ? (c1 - c0 - part - 1) / parts + 1 : 0;   // results of this warp
+#pragma unroll 1
+            for (int k0 = 0; k0 < mine; k0 += 32, base += 32 * step) {
+                const int count = min(32, mine - k0);
                 float2 ml = make_float2(kNoMax, 0.0f);
-                if (mine <= c1) ml = __ldcg(reinterpret_cast<const float2*>(slot_of(mine) + p.group * kHeadDim + 2 * hq));
+                if (lane < count) ml = __ldcg(reinterpret_cast<const float2*>(base + lane * step + ml_at));
+                float4 x[16];   // sixteen results in flight
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (j < count) x[j] = __ldcg(reinterpret_cast<const float4*>(base + j * step + o_at));
                 const float top = fmaxf(m, warp_max(ml.x)), f = fast_exp2(ml.x - top), again = fast_exp2(m - top);
                 m = top;
                 l = l * again + warp_sum(f * ml.y);
                 o = make_float4(o.x * again, o.y * again, o.z * again, o.w * again);
-                const int count = min(32, (c1 - c) / parts + 1);
-                for (int k = 0; k < count; k += 8) {   // eight results in flight
-                    float4 x[8];
+#pragma unroll 1
+                for (int k = 0;;) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (k + j < count) x[j] = __ldcg(reinterpret_cast<const float4*>(slot_of(c + (k + j) * parts) + hq * kHeadDim) + lane);
-                    }
+                    for (int j = 0; j < 16; ++j)
+                        if (k + j < count) fma4(o, __shfl_sync(0xffffffffu, f, k + j), x[j]);
+                    if ((k += 16) >= count) break;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) fma4(o, __shfl_sync(0xffffffffu, f, (k + j) & 31), x[j]);
+                    for (int j = 0; j < 16; ++j)
+                        if (k + j < count) x[j] = __ldcg(reinterpret_cast<const float4*>(base + (k + j) * step + o_at));
                 }
             }
             *reinterpret_cast<float4*>(rows + warp * kRow + 4 * lane) = o;
@@ -523,18 +555,21 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
     }
 }
 
-int decode_grid(long long units, int max_pages, int num_sms) {
-    const long long most = (units * max_pages + kWarps * kMinPages - 1) / (kWarps * kMinPages);
-    return (int)std::max(1LL, std::min<long long>(num_sms, most));
-}
-
-size_t arrived_bytes(int num_sms) { return ((size_t)num_sms * sizeof(int) + 255) & ~(size_t)255; }
+struct DecodeGrid {
+    int ctas;
+    bool by_head;
+    DecodeGrid(int batch, int num_kv_heads, int max_pages, int num_sms) {
+        const long long most = ((long long)batch * num_kv_heads * max_pages + kWarps * kMinPages - 1) / (kWarps * kMinPages);
+        ctas = (int)std::max(1LL, std::min<long long>(num_sms, most));
+        by_head = num_kv_heads <= num_sms && (batch == 1 || num_sms % num_kv_heads == 0);
+        if (by_head) ctas = std::max(num_kv_heads, ctas / num_kv_heads * num_kv_heads);
+    }
+};
 
 }  // namespace
 
-size_t block_decode_workspace(int batch, int num_kv_heads, int group, int max_pages, int num_sms) {
-    const long long units = (long long)std::min(batch, kDecodeBatch) * num_kv_heads;
-    return arrived_bytes(num_sms) + sizeof(float) * (size_t)decode_grid(units, max_pages, num_sms) * (2 + kWarps) * slot_floats(group);
+size_t block_decode_workspace(int group, int num_sms) {   // the grid never exceeds the SMs
+    return sizeof(float) * (size_t)num_sms * (2 + kWarps) * slot_floats(group);
 }
 
 cudaError_t launch_block_decode(const BlockAttentionParams& params, int code, int num_sms, cudaStream_t stream) {
@@ -558,11 +593,11 @@ cudaError_t launch_block_decode(const BlockAttentionParams& params, int code, in
         p.ctx_lens = params.ctx_lens + b0;
         p.out = static_cast<uint16_t*>(params.out) + (size_t)b0 * params.num_q_heads * kHeadDim;
         p.lse = params.lse ? params.lse + (size_t)b0 * params.num_q_heads : nullptr;
-        const long long units = (long long)p.batch * p.num_kv_heads;
-        const int grid = decode_grid(units, p.max_pages, num_sms);
+        const DecodeGrid grid(p.batch, p.num_kv_heads, p.max_pages, num_sms);
+        args.by_head = grid.by_head;
         args.arrived = reinterpret_cast<int*>(p.partials);
-        args.partials = p.partials + arrived_bytes(num_sms) / sizeof(float);
-        if (cudaError_t e = launch_pdl(kernel, dim3(grid), dim3(kThreads), kSmem, stream, args)) return e;
+        args.partials = p.partials + block_arrived_bytes(num_sms) / sizeof(float);
+        if (cudaError_t e = launch_pdl(kernel, dim3(grid.ctas), dim3(kThreads), kSmem, stream, args)) return e;
     }
     return cudaSuccess;
 }

@@ -1,0 +1,576 @@
+// Attention of several query tokens per sequence over the block-scaled cache.
+//
+// A CTA takes two tiles of 128 rows (query tokens x the G query heads of one KV head, token major) and
+// walks the context in tiles of 128 keys (8 pages).  Both products run on the fifth-generation tensor
+// cores with accumulators in TMEM:
+//   S = Q K^T   both operands in shared memory, K's codes expanded to exact fp16
+//   O += P V    P (fp16) from TMEM, in S's columns; V's codes as exact fp16 in shared memory
+// Page scales stay out of the operands: with y = S ks + log2(vs) (ks the page's key scale times
+// softmax_scale log2(e) and the row's query factor) 2^(y - m) is p vs, so O sums it times V's codes, and
+// the sum of weights takes 2^(y - m) / vs.
+// Warps 0-3 and 4-7: softmax of a tile each, a row per thread, one tile's while the tensor cores work on
+// the other's; warps 8-11: codes from global memory to fp16 operands, two stages; warp 12: the MMAs.
+// A softmax thread moves its running maximum (and its row of O) only when a logit passes it by 2^8.
+#include "block_common.cuh"
+#include "decode_common.cuh"
+
+namespace wc {
+
+namespace {
+
+constexpr int kTile = 128;                 // rows of a query tile, keys of a context tile
+constexpr int kPages = kTile / kPage;      // pages of a context tile
+constexpr int kTiles = 2;                  // query tiles of a CTA
+constexpr int kSoftmaxWarps = 4 * kTiles, kConvertWarps = 4;
+constexpr int kMmaWarp = kSoftmaxWarps + kConvertWarps;
+constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kOperand = kTile * kHeadDim * 2;   // bytes of a [128][128] fp16 operand: two blocks of 64 channels
+constexpr int kBlock = kOperand / 2;
+constexpr int kMetaStages = 4;
+constexpr float kNoMax = -1e30f;
+constexpr float kSlack = 8.0f;
+constexpr uint32_t kTmemColumns = 512, kOutColumn = 256;   // S (and P) of tile t at 128 t, O at 256 + 128 t
+
+struct Meta {   // of a context tile's pages
+    float ks[kPages], bias[kPages], inv[kPages];
+};
+
+struct Shared {
+    uint64_t q_full, drained, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[kTiles], p_full[kTiles], o_full[kTiles];
+    Meta meta[kMetaStages];
+    uint32_t tmem;
+    int abandoned;
+};
+constexpr int kSmem = (kTiles + 4) * kOperand + (int)sizeof(Shared) + 1024;
+
+struct ExtendArgs {
+    BlockAttentionParams p;
+    int splits;
+    float* part_o;    // [splits][n_tok * Hq][128]
+    float2* part_ml;  // [splits][n_tok * Hq]
+};
+
+// ---- tcgen05 ------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* dst) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "r"(kTmemColumns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t tmem) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns));
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint64_t* bar) {   // bar is arrived at when all MMAs so far are done
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// D (128 x 128 fp32) = or += A B, 16 deep.  Operand descriptors below.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// Shared-memory operand with the 128-byte swizzle: rows of 64 channels, 8 rows in 1024 bytes.  Q and K: channels are the
+// summed dimension, 64 of them a block.  V: keys are; the leading offset leads to the block of the next 64 channels.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
+    return (uint64_t)(addr >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp16 operands, fp32 accumulator, 128 x 128; bit 16: B's rows are the summed dimension (V).
+constexpr uint32_t kIdescQk = 1u << 4 | (kTile >> 3) << 17 | (kTile >> 4) << 24, kIdescPv = kIdescQk | 1u << 16;
+
+__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Bounded wait; once one gives up, all do.
+__device__ __forceinline__ bool wait(Shared& s, uint64_t* bar, uint32_t parity) {
+    for (int i = 0; i < kMaxWaitTries; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*reinterpret_cast<volatile int*>(&s.abandoned)) return false;
+    }
+    *reinterpret_cast<volatile int*>(&s.abandoned) = 1;
+    return false;
+}
+
+// ---- work ---------------------------------------------------------------------------------------
+
+// A CTA's rows: n_rows (token, query head) rows from `row0` of sequence b, which has n query rows from
+// token `lo` on and ctx keys.
+struct Work {
+    int b, lo, n, ctx, row0, rows;
+};
+
+// Blocks first(b) = cu[b] G / 256 + b on are sequence b's (one more than its whole tile pairs).
+__device__ __forceinline__ bool find_work(const BlockAttentionParams& p, int block, Work& w) {
+    int tile;
+    if (p.cu_q) {
+        auto first = [&](int s) { return ((long long)load_dep(p.cu_q + s) * p.group) / (kTiles * kTile) + s; };
+        w.b = warp_find_last(p.batch, block, first);
+        tile = block - (int)first(w.b);
+        w.lo = load_dep(p.cu_q + w.b);
+        const int hi = load_dep(p.cu_q + w.b + 1);
+        if (w.lo < 0 || hi < w.lo || hi > p.n_tok || tile < 0) return false;
+        w.n = hi - w.lo;
+    } else {
+        w.b = w.lo = block;
+        w.n = 1;
+        tile = 0;
+    }
+    const long long row0 = (long long)tile * (kTiles * kTile), all = (long long)w.n * p.group;
+    if (row0 >= all) return false;
+    w.row0 = (int)row0;
+    w.rows = (int)min((long long)(kTiles * kTile), all - row0);
+    w.ctx = load_dep(p.ctx_lens + w.b);
+    if (w.ctx < 0 || w.ctx > (long long)p.max_pages * kPage) {
+        if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, WC_DEV_BAD_CTX);
+        w.ctx = 0;
+    }
+    return true;
+}
+
+// Keys that row r of the sequence sees (those below).
+__device__ __forceinline__ int keys_seen(const BlockAttentionParams& p, const Work& w, int r) {
+    return p.causal ? max(0, min(w.ctx, w.ctx - w.n + r / p.group + 1)) : w.ctx;
+}
+
+// One half of a softmax step on 32 columns of a row, two pages of keys.
+template <bool kMask>
+__device__ __forceinline__ float page_max(const uint32_t* r, int at, int seen) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPage; ++i) {
+        const float x = __uint_as_float(r[i]);
+        top = fmaxf(top, !kMask || at + i < seen ? x : -INFINITY);
+    }
+    return top;
+}
+
+template <int kCode>
+__global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_constant__ ExtendArgs args) {
+    const BlockAttentionParams& p = args.p;
+    extern __shared__ uint8_t raw[];
+    uint8_t* ops = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *q_op = ops, *k_op = ops + kTiles * kOperand, *v_op = k_op + 2 * kOperand;
+    Shared& s = *reinterpret_cast<Shared*>(v_op + 2 * kOperand);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, head = blockIdx.y;
+    if (threadIdx.x == 0) {
+        mbar_init(&s.q_full, kSoftmaxWarps * 32);
+        mbar_init(&s.drained, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.k_full[i], kConvertWarps * 32);
+            mbar_init(&s.v_full[i], kConvertWarps * 32);
+            mbar_init(&s.k_empty[i], 1);
+            mbar_init(&s.v_empty[i], 1);
+            mbar_init(&s.s_full[i], 1);
+            mbar_init(&s.p_full[i], 128);
+            mbar_init(&s.o_full[i], 1);
+        }
+        s.abandoned = 0;
+        fence_barrier_init();
+    }
+    grid_dep_wait();
+    grid_dep_launch();
+    if (p.cu_q && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0)   // one CTA reports the ranges that cannot be
+        for (int i = threadIdx.x; i < p.batch; i += kThreads) {
+            const int x = load_dep(p.cu_q + i), y = load_dep(p.cu_q + i + 1);
+            if (x < 0 || y < x || y > p.n_tok) atomicOr(p.status, WC_DEV_BAD_ROWS);
+        }
+    Work w;
+    // the blocks of a sequence's last rows come first: with a causal mask theirs is the most work
+    if (!find_work(p, gridDim.x - 1 - blockIdx.x, w)) return;
+    const int tiles_q = w.rows > kTile ? 2 : 1;
+    const int keys = keys_seen(p, w, w.row0 + w.rows - 1), context_tiles = (keys + kTile - 1) / kTile;
+    const int t0 = (int)((long long)context_tiles * blockIdx.z / args.splits);
+    const int t1 = (int)((long long)context_tiles * (blockIdx.z + 1) / args.splits), n = t1 - t0;
+    if (warp == kMmaWarp && n > 0) tmem_alloc(&s.tmem);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = n > 0 ? s.tmem : 0;
+
+    if (warp < kSoftmaxWarps) {
+        const int t = warp >> 2, thread = threadIdx.x & 127, r = w.row0 + t * kTile + thread;
+        const bool live = t * kTile + thread < w.rows;
+        const int token = r / p.group, hq = head * p.group + r - token * p.group;
+        const size_t cell = (size_t)(w.lo + token) * p.num_q_heads + hq;
+        float m = kNoMax, l = 0.0f;
+        float* part = args.splits > 1 ? args.part_o + ((size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell) * kHeadDim : nullptr;
+        bool ok = true;
+        if (n > 0) {
+            // the row of Q: bf16 scaled by a power of two into fp16's range
+            uint32_t q[64];
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) + (size_t)(w.lo + token) * p.q_stride + (size_t)hq * kHeadDim);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint4 x = live ? load_dep(src + i) : make_uint4(0, 0, 0, 0);
+                q[4 * i] = x.x, q[4 * i + 1] = x.y, q[4 * i + 2] = x.z, q[4 * i + 3] = x.w;
+            }
+            const float factor = p.bf16 ? bf16_row_to_f16(q, [](uint32_t x) { return x; }) : 1.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                *reinterpret_cast<uint4*>(q_op + t * kOperand + (i >> 3) * kBlock + thread * 128 + 16 * ((i & 7) ^ (thread & 7))) =
+                    make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+            fence_async();
+            arrive(&s.q_full);
+
+            const int seen = live ? keys_seen(p, w, r) : 0;
+            const int least = __reduce_min_sync(0xffffffffu, live ? seen : w.ctx);   // of the warp's rows
+            const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + t * kTile + lanes, o_at = tmem + kOutColumn + t * kTile + lanes;
+            if (t < tiles_q) {
+                for (int j = 0; j < n && ok; ++j) {
+                    ok = wait(s, &s.s_full[t], j & 1);   // and the O += P V before it is done
+                    if (!ok) break;
+                    fence_after();
+                    const Meta& meta = s.meta[j % kMetaStages];
+                    const int key0 = (t0 + j) * kTile, sees = seen - key0;
+                    const bool masked = least < key0 + kTile;
+                    float top = kNoMax;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[32];
+                        tmem_ld32(s_at + 32 * c, x);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float best = masked ? page_max<true>(x + 16 * h, 32 * c + 16 * h, sees) : page_max<false>(x + 16 * h, 0, 0);
+                            top = fmaxf(top, fmaf(best, meta.ks[2 * c + h] * factor, meta.bias[2 * c + h]));
+                        }
+                    }
+                    if (__any_sync(0xffffffffu, top > m + kSlack)) {
+                        const float now = fmaxf(m, top), f = fast_exp2(m - now);
+                        m = now;
+                        l *= f;
+                        if (j > 0) {
+#pragma unroll 1
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t x[32];
+                                tmem_ld32(o_at + 32 * c, x);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+                                tmem_st32(o_at + 32 * c, x);
+                            }
+                            tmem_wait_st();
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[32], y[16];
+                        tmem_ld32(s_at + 32 * c, x);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float ks = meta.ks[2 * c + h] * factor, bias = meta.bias[2 * c + h] - m;
+                            float sum = 0.0f;
+#pragma unroll
+                            for (int i = 0; i < kPage; i += 2) {
+                                float a = fast_exp2(fmaf(__uint_as_float(x[16 * h + i]), ks, bias));
+                                float b = fast_exp2(fmaf(__uint_as_float(x[16 * h + i + 1]), ks, bias));
+                                if (masked) {
+                                    a = 32 * c + 16 * h + i < sees ? a : 0.0f;
+                                    b = 32 * c + 16 * h + i + 1 < sees ? b : 0.0f;
+                                }
+                                sum += a + b;
+                                y[8 * h + i / 2] = pack_h2(a, b);
+                            }
+                            l = fmaf(sum, meta.inv[2 * c + h], l);
+                        }
+                        tmem_st16(s_at + 16 * c, y);   // P takes the place of S's columns that have been read
+                    }
+                    tmem_wait_st();
+                    fence_before();
+                    arrive(&s.p_full[t]);
+                }
+                ok = ok && wait(s, &s.o_full[t], 0);
+                fence_after();
+                if (ok) {
+                    const float f = part ? 1.0f : l == 0.0f ? 0.0f : __frcp_rn(l);
+                    uint16_t* out = static_cast<uint16_t*>(p.out) + cell * kHeadDim;
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[32];
+                        tmem_ld32(o_at + 32 * c, x);
+                        tmem_wait_ld();
+                        if (live && part) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                reinterpret_cast<uint4*>(part + 32 * c)[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                        } else if (live) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t o[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    const float a = l == 0.0f ? 0.0f : __uint_as_float(x[8 * i + 2 * k]) * f;
+                                    const float b = l == 0.0f ? 0.0f : __uint_as_float(x[8 * i + 2 * k + 1]) * f;
+                                    o[k] = p.bf16 ? float2_to_act2<true>(a, b) : pack_h2(a, b);
+                                }
+                                reinterpret_cast<uint4*>(out + 32 * c)[i] = make_uint4(o[0], o[1], o[2], o[3]);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+        } else if (live && !part) {   // no key in sight
+            uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + cell * kHeadDim);
+            for (int i = 0; i < 16; ++i) out[i] = make_uint4(0, 0, 0, 0);
+        }
+        if (live) {
+            if (part) args.part_ml[(size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell] = make_float2(m, l);
+            else if (p.lse) p.lse[cell] = log_sum(m, l);
+        }
+        if (!ok && lane == 0) atomicOr(p.status, WC_DEV_TIMEOUT);
+        fence_before();
+    } else if (warp < kMmaWarp) {
+        // keys and values: a warp looks after two pages of the tile, in steps of 4 rows (8 lanes a row, 16 codes a lane)
+        const int cw = warp - kSoftmaxWarps, sub = lane >> 3, chunk = lane & 7;
+        const int32_t* table = p.block_table + (size_t)w.b * p.max_pages;
+        const int pages = (w.ctx + kPage - 1) >> 4;
+        auto page_at = [&](int tile, int h) {   // -1: past the context, -2: outside the pool
+            const int page = tile * kPages + 2 * cw + h;
+            if (tile >= t1 || page >= pages) return -1;
+            const int phys = load_dep(table + page);
+            return phys < 0 || phys >= p.num_pages ? -2 : phys;
+        };
+        auto load = [&](const uint8_t* codes, const int (&phys)[2], uint4 (&x)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int ph = phys[i >> 2];
+                const size_t at = ((size_t)ph * p.num_kv_heads + head) * (kPage * kHeadDim) + (4 * (i & 3) + sub) * kHeadDim + 16 * chunk;
+                x[i] = ph >= 0 ? load_dep(reinterpret_cast<const uint4*>(codes + at)) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        auto store = [&](uint8_t* op, const uint4 (&x)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = 32 * cw + 4 * i + sub;
+                uint32_t h[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) codes4_to_h2<kCode>(word_of(x[i], k), h[2 * k], h[2 * k + 1]);
+                // lanes of the second block of channels store their odd half first: eight banks groups at a time
+                uint8_t* at = op + (chunk >> 2) * kBlock + row * 128;
+                const int c0 = 2 * (chunk & 3), odd = chunk >> 2;
+                const uint4 a = make_uint4(h[0], h[1], h[2], h[3]), b = make_uint4(h[4], h[5], h[6], h[7]);
+                *reinterpret_cast<uint4*>(at + 16 * ((c0 + odd) ^ (row & 7))) = odd ? b : a;
+                *reinterpret_cast<uint4*>(at + 16 * ((c0 + 1 - odd) ^ (row & 7))) = odd ? a : b;
+            }
+        };
+        if (n > 0) {
+            int phys[2], next[2];
+            uint4 kx[8], vx[8];
+            for (int h = 0; h < 2; ++h) phys[h] = page_at(t0, h), next[h] = page_at(t0 + 1, h);
+            load(p.codes[0], phys, kx);
+            load(p.codes[1], phys, vx);
+            bool ok = true;
+            for (int j = 0; j < n && ok; ++j) {
+                const int st = j & 1;
+                if (j >= 2) ok = wait(s, &s.k_empty[st], ((j >> 1) - 1) & 1);
+                if (!ok) break;
+                bool no_values[2];
+                float vs[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const size_t at = (size_t)max(phys[h], 0) * p.num_kv_heads + head;
+                    vs[h] = phys[h] >= 0 && p.scale[1] ? load_dep(p.scale[1] + at) : 1.0f;
+                    no_values[h] = vs[h] == 0.0f;
+                    if (no_values[h]) vs[h] = 1.0f;
+                    if (lane == h) {
+                        Meta& meta = s.meta[j % kMetaStages];
+                        const float ks = phys[h] >= 0 && p.scale[0] ? load_dep(p.scale[0] + at) : 1.0f;
+                        meta.ks[2 * cw + h] = ks * p.scale_log2;
+                        meta.bias[2 * cw + h] = phys[h] == -2 ? -INFINITY : log2f(vs[h]);
+                        meta.inv[2 * cw + h] = __frcp_rn(vs[h]);
+                        if (phys[h] == -2) atomicOr(p.status, WC_DEV_BAD_PAGE);
+                    }
+                }
+                store(k_op + st * kOperand, kx);
+                fence_async();
+                arrive(&s.k_full[st]);
+                load(p.codes[0], next, kx);
+                if (j >= 2) ok = wait(s, &s.v_empty[st], ((j >> 1) - 1) & 1);
+                if (!ok) break;
+                // codes past the context, or of a page with scale 0, must not count (NaN among them)
+                const int have = w.ctx - (t0 + j) * kTile;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (no_values[i >> 2] || 32 * cw + 4 * i + sub >= have) vx[i] = make_uint4(0, 0, 0, 0);
+                store(v_op + st * kOperand, vx);
+                fence_async();
+                arrive(&s.v_full[st]);
+                load(p.codes[1], next, vx);
+                for (int h = 0; h < 2; ++h) phys[h] = next[h], next[h] = page_at(t0 + j + 2, h);
+            }
+        }
+    } else if (n > 0) {
+        bool ok = true;
+        if (elect_one()) {
+            const uint32_t q_addr = smem_addr(q_op), k_addr = smem_addr(k_op), v_addr = smem_addr(v_op);
+            auto qk = [&](int t, int st) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t off = (i >> 2) * kBlock + (i & 3) * 32;
+                    mma_ss(tmem + t * kTile, operand(q_addr + t * kOperand + off, 16), operand(k_addr + st * kOperand + off, 16), kIdescQk, i > 0);
+                }
+                commit(&s.s_full[t]);
+            };
+            ok = wait(s, &s.q_full, 0) && wait(s, &s.k_full[0], 0);
+            if (ok) {
+                fence_after();
+                for (int t = 0; t < tiles_q; ++t) qk(t, 0);
+                commit(&s.k_empty[0]);
+            }
+            for (int j = 0; j < n && ok; ++j) {
+                const int st = j & 1;
+                ok = wait(s, &s.v_full[st], (j >> 1) & 1);
+                for (int t = 0; t < tiles_q && ok; ++t) {
+                    ok = wait(s, &s.p_full[t], j & 1);
+                    if (!ok) break;
+                    fence_after();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)   // 16 keys each: 8 columns of P, 16 rows of V
+                        mma_ts(tmem + kOutColumn + t * kTile, tmem + t * kTile + 8 * i, operand(v_addr + st * kOperand + i * 2048, kBlock), kIdescPv,
+                               j > 0 || i > 0);
+                    if (j + 1 < n) {
+                        if (t == 0) ok = wait(s, &s.k_full[st ^ 1], ((j + 1) >> 1) & 1);
+                        if (!ok) break;
+                        fence_after();
+                        qk(t, st ^ 1);
+                    } else {
+                        commit(&s.o_full[t]);
+                    }
+                }
+                if (ok) {
+                    commit(&s.v_empty[st]);
+                    if (j + 1 < n) commit(&s.k_empty[st ^ 1]);
+                }
+            }
+            if (!ok) {   // what was issued ends before the accumulators are given back
+                commit(&s.drained);
+                (void)mbar_wait_bounded(&s.drained, 0);
+            }
+        }
+        __syncwarp();
+    }
+    __syncthreads();
+    if (warp == kMmaWarp && n > 0) {
+        fence_after();
+        tmem_free(tmem);
+    }
+}
+
+// Splits of a row merged: a warp per row, four channels a lane.
+__global__ void __launch_bounds__(256) block_extend_merge_kernel(const __grid_constant__ ExtendArgs args) {
+    const BlockAttentionParams& p = args.p;
+    grid_dep_wait();
+    grid_dep_launch();
+    const int lane = threadIdx.x & 31;
+    const size_t cells = (size_t)p.n_tok * p.num_q_heads, cell = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (cell >= cells) return;
+    if (p.cu_q) {   // rows outside every sequence's range are not written
+        const int row = (int)(cell / p.num_q_heads);
+        const int b = warp_find_last(p.batch, row, [&](int s) { return (long long)load_dep(p.cu_q + s); });
+        const int lo = load_dep(p.cu_q + b), hi = load_dep(p.cu_q + b + 1);
+        if (lo < 0 || hi > p.n_tok || row < lo || row >= hi) return;
+    }
+    float m = kNoMax, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = 0; i < args.splits; ++i) {
+        const float2 ml = args.part_ml[i * cells + cell];
+        if (ml.y == 0.0f) continue;   // no key in sight: its sums were not written
+        const float4 x = reinterpret_cast<const float4*>(args.part_o + (i * cells + cell) * kHeadDim)[lane];
+        const float now = fmaxf(m, ml.x), f = fast_exp2(m - now), g = fast_exp2(ml.x - now);
+        m = now;
+        l = l * f + g * ml.y;
+        o.x = o.x * f + g * x.x;
+        o.y = o.y * f + g * x.y;
+        o.z = o.z * f + g * x.z;
+        o.w = o.w * f + g * x.w;
+    }
+    store_output(p, cell, lane, o, m, l);
+}
+
+constexpr int kMaxSplits = 64, kMaxCtas = 4;   // of a row; of a call that splits rows, per SM
+
+struct ExtendPlan {
+    long long blocks;   // tile pairs, an upper bound
+    int splits;
+    ExtendPlan(int batch, int n_tok, int num_kv_heads, int group, int max_pages, int num_sms) {
+        blocks = std::min<long long>((long long)n_tok * group / (kTiles * kTile) + batch, n_tok);
+        // the split count that takes the fewest tile steps: waves x (tiles of a split + a fixed part of about two)
+        const long long ctas = blocks * num_kv_heads;
+        const int tiles = (max_pages + kPages - 1) / kPages;
+        long long best = -1;
+        splits = 1;
+        for (int s = 1; s <= std::min(tiles, kMaxSplits) && (s == 1 || ctas * s <= (long long)kMaxCtas * num_sms); ++s) {
+            const long long waves = (ctas * s + num_sms - 1) / num_sms, cost = waves * ((tiles + s - 1) / s + 2) + (s > 1 ? 2 : 0);
+            if (best < 0 || cost < best) best = cost, splits = s;
+        }
+    }
+};
+
+size_t part_ml_bytes(long long cells, int splits) { return ((size_t)cells * splits * sizeof(float2) + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// For calls of up to n_tok tokens, whatever their batch and context: a CTA holds at most two tiles of rows.
+size_t block_extend_workspace(int n_tok, int num_q_heads, int num_sms) {
+    const long long rows = std::min((long long)n_tok * num_q_heads * kMaxSplits, (long long)kTiles * kTile * kMaxCtas * num_sms);
+    return part_ml_bytes(rows, 1) + (size_t)rows * kHeadDim * sizeof(float);
+}
+
+cudaError_t launch_block_extend(const BlockAttentionParams& p, int code, int num_sms, cudaStream_t stream) {
+    static PerDevice<Configured, cudaError_t> configured[2];
+    auto* kernel = code == WC_CODE_INT8 ? block_extend_kernel<WC_CODE_INT8> : block_extend_kernel<WC_CODE_E4M3>;
+    if (cudaError_t e = configure(configured[code == WC_CODE_INT8], kernel, kSmem)) return e;
+    const ExtendPlan plan(p.batch, p.n_tok, p.num_kv_heads, p.group, p.max_pages, num_sms);
+    const long long cells = (long long)p.n_tok * p.num_q_heads;
+    ExtendArgs args;
+    args.p = p;
+    args.splits = plan.splits;
+    float* scratch = p.partials + block_arrived_bytes(num_sms) / sizeof(float);
+    args.part_ml = reinterpret_cast<float2*>(scratch);
+    args.part_o = scratch + part_ml_bytes(cells, plan.splits) / sizeof(float);
+    if (cudaError_t e = launch_pdl(kernel, dim3((unsigned)plan.blocks, p.num_kv_heads, plan.splits), dim3(kThreads), kSmem, stream, args))
+        return e;
+    if (plan.splits == 1) return cudaSuccess;
+    static PerDevice<Configured, cudaError_t> merge_configured;
+    if (cudaError_t e = configure(merge_configured, block_extend_merge_kernel, 0)) return e;
+    return launch_pdl(block_extend_merge_kernel, dim3((unsigned)((cells + 7) / 8)), dim3(256), 0, stream, args);
+}
+
+}  // namespace wc
