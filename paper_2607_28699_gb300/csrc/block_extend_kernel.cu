@@ -23,7 +23,11 @@ constexpr int kPages = kTile / kPage;      // pages of a context tile
 constexpr int kTiles = 2;                  // query tiles of a CTA
 constexpr int kSoftmaxWarps = 4 * kTiles, kConvertWarps = 4;
 constexpr int kMmaWarp = kSoftmaxWarps + kConvertWarps;
-constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kThreads = 32 * (kMmaWarp + 4);
+// Registers: 128 a thread at launch, 512 threads; a softmax thread holds 64 packed weights and 32 logits and
+// takes what the MMA warps give: 256 x 176 + 128 x 128 + 128 x 32 = 512 x 128.
+constexpr int kSoftmaxRegs = 176, kMmaRegs = 32;
+static_assert(kSoftmaxWarps * 32 * kSoftmaxRegs + kConvertWarps * 32 * 128 + 4 * 32 * kMmaRegs <= kThreads * 128);
 constexpr int kOperand = kTile * kHeadDim * 2;   // bytes of a [128][128] fp16 operand: two blocks of 64 channels
 constexpr int kBlock = kOperand / 2;
 constexpr int kMetaStages = 4;
@@ -101,13 +105,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) 
         "r"(r[31])
         : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -167,16 +164,52 @@ __device__ __forceinline__ int keys_seen(const BlockAttentionParams& p, const Wo
     return p.causal ? max(0, min(w.ctx, w.ctx - w.n + r / p.group + 1)) : w.ctx;
 }
 
-// One half of a softmax step on 32 columns of a row, two pages of keys.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// A row's weights for a context tile under the maximum m: pairs as fp16 in y, their sum (in units of the
+// weights p: value scales divided out) returned; top: the tile's largest exponent.  kMask: the row sees the first
+// `sees` keys of the tile only.
 template <bool kMask>
-__device__ __forceinline__ float page_max(const uint32_t* r, int at, int seen) {
-    float top = -INFINITY;
+__device__ __forceinline__ float weights(uint32_t s_at, const Meta& meta, float factor, float m, int sees, uint32_t (&y)[kTile / 2], float& top) {
+    float l = 0.0f;
+    top = kNoMax;
 #pragma unroll
-    for (int i = 0; i < kPage; ++i) {
-        const float x = __uint_as_float(r[i]);
-        top = fmaxf(top, !kMask || at + i < seen ? x : -INFINITY);
+    for (int c = 0; c < 4; ++c) {
+        uint32_t x[32];
+        tmem_ld32(s_at + 32 * c, x);
+        tmem_wait_ld();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int page = 2 * c + h;
+            const float ks = meta.ks[page] * factor, bias = meta.bias[page], shift = bias - m;
+            const float2 ks2 = make_float2(ks, ks), shift2 = make_float2(shift, shift);
+            float best = -INFINITY;
+            float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < kPage; i += 2) {
+                const float2 v = make_float2(__uint_as_float(x[16 * h + i]), __uint_as_float(x[16 * h + i + 1]));
+                const float2 e = __ffma2_rn(v, ks2, shift2);
+                float2 pr = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+                if constexpr (kMask) {
+                    const bool in0 = 16 * page + i < sees, in1 = 16 * page + i + 1 < sees;
+                    best = max3(best, in0 ? v.x : -INFINITY, in1 ? v.y : -INFINITY);
+                    pr.x = in0 ? pr.x : 0.0f;
+                    pr.y = in1 ? pr.y : 0.0f;
+                } else {
+                    best = max3(best, v.x, v.y);
+                }
+                sum = __fadd2_rn(sum, pr);
+                y[8 * page + i / 2] = pack_h2(pr.x, pr.y);
+            }
+            top = fmaxf(top, fmaf(best, ks, bias));
+            l = fmaf(sum.x + sum.y, meta.inv[page], l);
+        }
     }
-    return top;
+    return l;
 }
 
 template <int kCode>
@@ -223,6 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     const uint32_t tmem = n > 0 ? s.tmem : 0;
 
     if (warp < kSoftmaxWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int t = warp >> 2, thread = threadIdx.x & 127, r = w.row0 + t * kTile + thread;
         const bool live = t * kTile + thread < w.rows;
         const int token = r / p.group, hq = head * p.group + r - token * p.group;
@@ -258,59 +292,30 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                     const Meta& meta = s.meta[j % kMetaStages];
                     const int key0 = (t0 + j) * kTile, sees = seen - key0;
                     const bool masked = least < key0 + kTile;
-                    float top = kNoMax;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32];
-                        tmem_ld32(s_at + 32 * c, x);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float best = masked ? page_max<true>(x + 16 * h, 32 * c + 16 * h, sees) : page_max<false>(x + 16 * h, 0, 0);
-                            top = fmaxf(top, fmaf(best, meta.ks[2 * c + h] * factor, meta.bias[2 * c + h]));
-                        }
-                    }
-                    if (__any_sync(0xffffffffu, top > m + kSlack)) {
+                    uint32_t y[kTile / 2];
+                    float sum;
+                    for (;;) {   // again where a logit passed the maximum by too much: in a row's first tile, then rarely
+                        float top;
+                        sum = masked ? weights<true>(s_at, meta, factor, m, sees, y, top) : weights<false>(s_at, meta, factor, m, sees, y, top);
+                        if (!__any_sync(0xffffffffu, top > m + kSlack)) break;
                         const float now = fmaxf(m, top), f = fast_exp2(m - now);
                         m = now;
                         l *= f;
-                        if (j > 0) {
+                        if (j == 0) continue;
 #pragma unroll 1
-                            for (int c = 0; c < 4; ++c) {
-                                uint32_t x[32];
-                                tmem_ld32(o_at + 32 * c, x);
-                                tmem_wait_ld();
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t x[32];
+                            tmem_ld32(o_at + 32 * c, x);
+                            tmem_wait_ld();
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
-                                tmem_st32(o_at + 32 * c, x);
-                            }
-                            tmem_wait_st();
+                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+                            tmem_st32(o_at + 32 * c, x);
                         }
                     }
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32], y[16];
-                        tmem_ld32(s_at + 32 * c, x);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float ks = meta.ks[2 * c + h] * factor, bias = meta.bias[2 * c + h] - m;
-                            float sum = 0.0f;
-#pragma unroll
-                            for (int i = 0; i < kPage; i += 2) {
-                                float a = fast_exp2(fmaf(__uint_as_float(x[16 * h + i]), ks, bias));
-                                float b = fast_exp2(fmaf(__uint_as_float(x[16 * h + i + 1]), ks, bias));
-                                if (masked) {
-                                    a = 32 * c + 16 * h + i < sees ? a : 0.0f;
-                                    b = 32 * c + 16 * h + i + 1 < sees ? b : 0.0f;
-                                }
-                                sum += a + b;
-                                y[8 * h + i / 2] = pack_h2(a, b);
-                            }
-                            l = fmaf(sum, meta.inv[2 * c + h], l);
-                        }
-                        tmem_st16(s_at + 16 * c, y);   // P takes the place of S's columns that have been read
-                    }
+                    l += sum;
+                    // P takes the place of S's first columns
+                    tmem_st32(s_at, reinterpret_cast<const uint32_t(&)[32]>(y[0]));
+                    tmem_st32(s_at + 32, reinterpret_cast<const uint32_t(&)[32]>(y[32]));
                     tmem_wait_st();
                     fence_before();
                     arrive(&s.p_full[t]);
@@ -436,9 +441,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 for (int h = 0; h < 2; ++h) phys[h] = next[h], next[h] = page_at(t0 + j + 2, h);
             }
         }
-    } else if (n > 0) {
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
         bool ok = true;
-        if (elect_one()) {
+        if (warp == kMmaWarp && n > 0 && elect_one()) {
             const uint32_t q_addr = smem_addr(q_op), k_addr = smem_addr(k_op), v_addr = smem_addr(v_op);
             auto qk = [&](int t, int st) {
 #pragma unroll
