@@ -25,8 +25,8 @@ constexpr int kSoftmaxWarps = 4 * kTiles, kConvertWarps = 4;
 constexpr int kMmaWarp = kSoftmaxWarps + kConvertWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 4);
 // Registers: 128 a thread at launch, 512 threads; a softmax thread holds 64 packed weights and 32 logits and
-// takes what the MMA warps give: 256 x 176 + 128 x 128 + 128 x 32 = 512 x 128.
-constexpr int kSoftmaxRegs = 176, kMmaRegs = 32;
+// takes what the MMA warps give: 256 x 168 + 128 x 128 + 128 x 48 = 512 x 128.
+constexpr int kSoftmaxRegs = 168, kMmaRegs = 48;
 static_assert(kSoftmaxWarps * 32 * kSoftmaxRegs + kConvertWarps * 32 * 128 + 4 * 32 * kMmaRegs <= kThreads * 128);
 constexpr int kOperand = kTile * kHeadDim * 2;   // bytes of a [128][128] fp16 operand: two blocks of 64 channels
 constexpr int kBlock = kOperand / 2;
@@ -79,8 +79,13 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 }
 // Shared-memory operand with the 128-byte swizzle: rows of 64 channels, 8 rows in 1024 bytes.  Q and K: channels are the
 // summed dimension, 64 of them a block.  V: keys are; the leading offset leads to the block of the next 64 channels.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
-    return (uint64_t)(addr >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// `low` is the descriptor's lower half (address and leading offset in units of 16 bytes).
+__device__ __forceinline__ uint32_t operand_low(const void* at, uint32_t leading) { return smem_addr(at) >> 4 | (leading >> 4) << 16; }
+__device__ __forceinline__ uint64_t operand(uint32_t low) {
+    constexpr uint32_t kHigh = (1024 >> 4) | 1u << 14 | 2u << 29;   // 8 rows' stride, version, swizzle
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "n"(kHigh));
+    return d;
 }
 // fp16 operands, fp32 accumulator, 128 x 128; bit 16: B's rows are the summed dimension (V).
 constexpr uint32_t kIdescQk = 1u << 4 | (kTile >> 3) << 17 | (kTile >> 4) << 24, kIdescPv = kIdescQk | 1u << 16;
@@ -113,11 +118,24 @@ __device__ __forceinline__ void arrive(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Bounded wait; once one gives up, all do.
+// Bounded wait (about two seconds); once one gives up, all do.
 __device__ __forceinline__ bool wait(Shared& s, uint64_t* bar, uint32_t parity) {
-    for (int i = 0; i < kMaxWaitTries; ++i) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (*reinterpret_cast<volatile int*>(&s.abandoned)) return false;
+    const uint32_t at = smem_addr(bar);
+    uint64_t since = 0;
+    for (uint32_t i = 1;; ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok)
+                     : "r"(at), "r"(parity)
+                     : "memory");
+        if (ok) return true;
+        if (i % 64 == 0) {
+            uint64_t now;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+            if (since == 0) since = now;
+            if (*reinterpret_cast<volatile int*>(&s.abandoned)) return false;
+            if (now - since > 2000000000ull) break;
+        }
     }
     *reinterpret_cast<volatile int*>(&s.abandoned) = 1;
     return false;
@@ -216,7 +234,7 @@ template <int kCode>
 __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_constant__ ExtendArgs args) {
     const BlockAttentionParams& p = args.p;
     extern __shared__ uint8_t raw[];
-    uint8_t* ops = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* ops = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     uint8_t *q_op = ops, *k_op = ops + kTiles * kOperand, *v_op = k_op + 2 * kOperand;
     Shared& s = *reinterpret_cast<Shared*>(v_op + 2 * kOperand);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, head = blockIdx.y;
@@ -362,8 +380,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         if (!ok && lane == 0) atomicOr(p.status, WC_DEV_TIMEOUT);
         fence_before();
     } else if (warp < kMmaWarp) {
-        // keys and values: a warp looks after two pages of the tile, in steps of 4 rows (8 lanes a row, 16 codes a lane)
-        const int cw = warp - kSoftmaxWarps, sub = lane >> 3, chunk = lane & 7;
+        // keys and values: a warp looks after two pages of the tile, 8 rows of 4 chunks of 16 codes at a time: 8 lanes in
+        // a row write to distinct banks of the swizzled operand, and all addresses are a lane's own plus constants
+        const int cw = warp - kSoftmaxWarps, row = lane & 7, chunk = lane >> 3;
+        const int src_at = row * kHeadDim + 16 * chunk, dst0 = (32 * cw + row) * 128 + 16 * ((2 * chunk) ^ row), dst1 = (32 * cw + row) * 128 + 16 * ((2 * chunk + 1) ^ row);
         const int32_t* table = p.block_table + (size_t)w.b * p.max_pages;
         const int pages = (w.ctx + kPage - 1) >> 4;
         auto page_at = [&](int tile, int h) {   // -1: past the context, -2: outside the pool
@@ -374,25 +394,24 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         };
         auto load = [&](const uint8_t* codes, const int (&phys)[2], uint4 (&x)[8]) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int ph = phys[i >> 2];
-                const size_t at = ((size_t)ph * p.num_kv_heads + head) * (kPage * kHeadDim) + (4 * (i & 3) + sub) * kHeadDim + 16 * chunk;
-                x[i] = ph >= 0 ? load_dep(reinterpret_cast<const uint4*>(codes + at)) : make_uint4(0, 0, 0, 0);
+            for (int h = 0; h < 2; ++h) {
+                const uint8_t* page = codes + ((size_t)max(phys[h], 0) * p.num_kv_heads + head) * (kPage * kHeadDim) + src_at;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[4 * h + i] = make_uint4(0, 0, 0, 0);
+                    if (phys[h] >= 0) x[4 * h + i] = load_dep(reinterpret_cast<const uint4*>(page + (i >> 1) * (8 * kHeadDim) + (i & 1) * 64));
+                }
             }
         };
         auto store = [&](uint8_t* op, const uint4 (&x)[8]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int row = 32 * cw + 4 * i + sub;
                 uint32_t h[8];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) codes4_to_h2<kCode>(word_of(x[i], k), h[2 * k], h[2 * k + 1]);
-                // lanes of the second block of channels store their odd half first: eight banks groups at a time
-                uint8_t* at = op + (chunk >> 2) * kBlock + row * 128;
-                const int c0 = 2 * (chunk & 3), odd = chunk >> 2;
-                const uint4 a = make_uint4(h[0], h[1], h[2], h[3]), b = make_uint4(h[4], h[5], h[6], h[7]);
-                *reinterpret_cast<uint4*>(at + 16 * ((c0 + odd) ^ (row & 7))) = odd ? b : a;
-                *reinterpret_cast<uint4*>(at + 16 * ((c0 + 1 - odd) ^ (row & 7))) = odd ? a : b;
+                uint8_t* at = op + (i & 1) * kBlock + (i >> 1) * 1024;
+                *reinterpret_cast<uint4*>(at + dst0) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4*>(at + dst1) = make_uint4(h[4], h[5], h[6], h[7]);
             }
         };
         if (n > 0) {
@@ -431,9 +450,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 if (!ok) break;
                 // codes past the context, or of a page with scale 0, must not count (NaN among them)
                 const int have = w.ctx - (t0 + j) * kTile;
+                if (have < kTile || no_values[0] || no_values[1]) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (no_values[i >> 2] || 32 * cw + 4 * i + sub >= have) vx[i] = make_uint4(0, 0, 0, 0);
+                    for (int i = 0; i < 8; ++i)
+                        if (no_values[i >> 2] || 32 * cw + 8 * (i >> 1) + row >= have) vx[i] = make_uint4(0, 0, 0, 0);
+                }
                 store(v_op + st * kOperand, vx);
                 fence_async();
                 arrive(&s.v_full[st]);
@@ -445,12 +466,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
         bool ok = true;
         if (warp == kMmaWarp && n > 0 && elect_one()) {
-            const uint32_t q_addr = smem_addr(q_op), k_addr = smem_addr(k_op), v_addr = smem_addr(v_op);
+            const uint32_t q_low = operand_low(q_op, 16), k_low = operand_low(k_op, 16), v_low = operand_low(v_op, kBlock);
             auto qk = [&](int t, int st) {
+                const uint32_t q = q_low + t * (kOperand >> 4), k = k_low + st * (kOperand >> 4), d = tmem + t * kTile;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint32_t off = (i >> 2) * kBlock + (i & 3) * 32;
-                    mma_ss(tmem + t * kTile, operand(q_addr + t * kOperand + off, 16), operand(k_addr + st * kOperand + off, 16), kIdescQk, i > 0);
+                    const uint32_t off = ((i >> 2) * kBlock + (i & 3) * 32) >> 4;
+                    mma_ss(d, operand(q + off), operand(k + off), kIdescQk, i > 0);
                 }
                 commit(&s.s_full[t]);
             };
@@ -467,10 +489,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                     ok = wait(s, &s.p_full[t], j & 1);
                     if (!ok) break;
                     fence_after();
+                    const uint32_t v = v_low + st * (kOperand >> 4), pr = tmem + t * kTile, d = pr + kOutColumn;
+                    mma_ts(d, pr, operand(v), kIdescPv, j > 0);   // 16 keys each: 8 columns of P, 16 rows of V
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)   // 16 keys each: 8 columns of P, 16 rows of V
-                        mma_ts(tmem + kOutColumn + t * kTile, tmem + t * kTile + 8 * i, operand(v_addr + st * kOperand + i * 2048, kBlock), kIdescPv,
-                               j > 0 || i > 0);
+                    for (int i = 1; i < 8; ++i) mma_ts(d, pr + 8 * i, operand(v + i * (2048 >> 4)), kIdescPv, true);
                     if (j + 1 < n) {
                         if (t == 0) ok = wait(s, &s.k_full[st ^ 1], ((j + 1) >> 1) & 1);
                         if (!ok) break;
