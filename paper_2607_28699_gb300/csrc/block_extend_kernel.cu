@@ -9,7 +9,9 @@
 // softmax_scale log2(e) and the row's query factor) 2^(y - m) is p vs, so O sums it times V's codes, and
 // the sum of weights takes 2^(y - m) / vs.
 // Warps 0-3 and 4-7: softmax of a tile each, a row per thread, one tile's while the tensor cores work on
-// the other's; warps 8-11: codes from global memory to fp16 operands, two stages; warp 12: the MMAs.
+// the other's; warps 8-11: codes to fp16 operands, two stages; warp 12: the MMAs.  The codes come to
+// shared memory by TMA, two pages a warp: read with ordinary loads in rows of 64 bytes, the shape in which
+// the operands are written without bank conflicts, they cost the MMAs' operand fetch a third of its time.
 // A softmax thread moves its running maximum (and its row of O) only when a logit passes it by 2^8.
 #include "block_common.cuh"
 #include "decode_common.cuh"
@@ -25,11 +27,12 @@ constexpr int kSoftmaxWarps = 4 * kTiles, kConvertWarps = 4;
 constexpr int kMmaWarp = kSoftmaxWarps + kConvertWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 4);
 // Registers: 128 a thread at launch, 512 threads; a softmax thread holds 64 packed weights and 32 logits and
-// takes what the MMA warps give: 256 x 168 + 128 x 128 + 128 x 48 = 512 x 128.
-constexpr int kSoftmaxRegs = 168, kMmaRegs = 48;
-static_assert(kSoftmaxWarps * 32 * kSoftmaxRegs + kConvertWarps * 32 * 128 + 4 * 32 * kMmaRegs <= kThreads * 128);
+// takes what the MMA warps give: 256 x 176 + 128 x 96 + 128 x 64 = 512 x 128.
+constexpr int kSoftmaxRegs = 176, kConvertRegs = 96, kMmaRegs = 64;
+static_assert(kSoftmaxWarps * 32 * kSoftmaxRegs + kConvertWarps * 32 * kConvertRegs + 4 * 32 * kMmaRegs <= kThreads * 128);
 constexpr int kOperand = kTile * kHeadDim * 2;   // bytes of a [128][128] fp16 operand: two blocks of 64 channels
 constexpr int kBlock = kOperand / 2;
+constexpr int kCodes = kTile * kHeadDim;         // bytes of a context tile's keys, or values
 constexpr int kMetaStages = 4;
 constexpr float kNoMax = -1e30f;
 constexpr float kSlack = 8.0f;
@@ -40,15 +43,18 @@ struct Meta {   // of a context tile's pages
 };
 
 struct Shared {
+    uint64_t codes[2][kConvertWarps];   // a warp's two pages of keys, of values are there
     uint64_t q_full, drained, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[kTiles], p_full[kTiles], o_full[kTiles];
     Meta meta[kMetaStages];
     uint32_t tmem;
     int abandoned;
 };
-constexpr int kSmem = (kTiles + 4) * kOperand + (int)sizeof(Shared) + 1024;
+constexpr int kSmem = (kTiles + 4) * kOperand + 2 * kCodes + (int)sizeof(Shared) + 1024;
+static_assert(kSmem <= 227 * 1024);
 
 struct ExtendArgs {
     BlockAttentionParams p;
+    CUtensorMap maps[2];   // keys, values
     int splits;
     float* part_o;    // [splits][n_tok * Hq][128]
     float2* part_ml;  // [splits][n_tok * Hq]
@@ -236,11 +242,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     extern __shared__ uint8_t raw[];
     uint8_t* ops = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     uint8_t *q_op = ops, *k_op = ops + kTiles * kOperand, *v_op = k_op + 2 * kOperand;
-    Shared& s = *reinterpret_cast<Shared*>(v_op + 2 * kOperand);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, head = blockIdx.y;
+    uint8_t* staged = v_op + 2 * kOperand;
+    Shared& s = *reinterpret_cast<Shared*>(staged + 2 * kCodes);
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, head = blockIdx.y;   // warp: uniform
     if (threadIdx.x == 0) {
         mbar_init(&s.q_full, kSoftmaxWarps * 32);
         mbar_init(&s.drained, 1);
+        for (int i = 0; i < 2 * kConvertWarps; ++i) mbar_init(&s.codes[0][i], 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.k_full[i], kConvertWarps * 32);
             mbar_init(&s.v_full[i], kConvertWarps * 32);
@@ -271,21 +279,28 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = n > 0 ? s.tmem : 0;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, n > 0 ? s.tmem : 0, 0);
 
     if (warp < kSoftmaxWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        const int t = warp >> 2, thread = threadIdx.x & 127, r = w.row0 + t * kTile + thread;
-        const bool live = t * kTile + thread < w.rows;
-        const int token = r / p.group, hq = head * p.group + r - token * p.group;
-        const size_t cell = (size_t)(w.lo + token) * p.num_q_heads + hq;
+        const int t = warp >> 2, thread = threadIdx.x & 127;
+        // the row's query token and head, and its output cell; not held over the loop
+        auto row_of = [&](int& token, size_t& cell) {
+            const int r = w.row0 + t * kTile + thread, i = r / p.group;
+            token = w.lo + i;
+            cell = (size_t)token * p.num_q_heads + head * p.group + r - i * p.group;
+            return t * kTile + thread < w.rows;
+        };
         float m = kNoMax, l = 0.0f;
-        float* part = args.splits > 1 ? args.part_o + ((size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell) * kHeadDim : nullptr;
         bool ok = true;
         if (n > 0) {
             // the row of Q: bf16 scaled by a power of two into fp16's range
             uint32_t q[64];
-            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) + (size_t)(w.lo + token) * p.q_stride + (size_t)hq * kHeadDim);
+            int token;
+            size_t cell;
+            const bool live = row_of(token, cell);
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) + (size_t)token * p.q_stride +
+                                                              (cell - (size_t)token * p.num_q_heads) * kHeadDim);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const uint4 x = live ? load_dep(src + i) : make_uint4(0, 0, 0, 0);
@@ -299,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
             fence_async();
             arrive(&s.q_full);
 
-            const int seen = live ? keys_seen(p, w, r) : 0;
+            const int seen = live ? keys_seen(p, w, w.row0 + t * kTile + thread) : 0;
             const int least = __reduce_min_sync(0xffffffffu, live ? seen : w.ctx);   // of the warp's rows
             const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + t * kTile + lanes, o_at = tmem + kOutColumn + t * kTile + lanes;
             if (t < tiles_q) {
@@ -340,132 +355,137 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 }
                 ok = ok && wait(s, &s.o_full[t], 0);
                 fence_after();
-                if (ok) {
-                    const float f = part ? 1.0f : l == 0.0f ? 0.0f : __frcp_rn(l);
-                    uint16_t* out = static_cast<uint16_t*>(p.out) + cell * kHeadDim;
+            }
+        }
+        int token;
+        size_t cell;
+        const bool live = row_of(token, cell);
+        const bool split = args.splits > 1;
+        const size_t part = (size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell;
+        if (ok && n > 0 && t < tiles_q) {
+            const float f = l == 0.0f ? 0.0f : __frcp_rn(l);
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32];
-                        tmem_ld32(o_at + 32 * c, x);
-                        tmem_wait_ld();
-                        if (live && part) {
+            for (int c = 0; c < 4; ++c) {
+                uint32_t x[32];
+                tmem_ld32(tmem + kOutColumn + t * kTile + ((uint32_t)(warp & 3) << 21) + 32 * c, x);
+                tmem_wait_ld();
+                if (live && split) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                reinterpret_cast<uint4*>(part + 32 * c)[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-                        } else if (live) {
+                    for (int i = 0; i < 8; ++i)
+                        reinterpret_cast<uint4*>(args.part_o + part * kHeadDim + 32 * c)[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                } else if (live) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t o[4];
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t o[4];
 #pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    const float a = l == 0.0f ? 0.0f : __uint_as_float(x[8 * i + 2 * k]) * f;
-                                    const float b = l == 0.0f ? 0.0f : __uint_as_float(x[8 * i + 2 * k + 1]) * f;
-                                    o[k] = p.bf16 ? float2_to_act2<true>(a, b) : pack_h2(a, b);
-                                }
-                                reinterpret_cast<uint4*>(out + 32 * c)[i] = make_uint4(o[0], o[1], o[2], o[3]);
-                            }
+                        for (int k = 0; k < 4; ++k) {
+                            const float a = l == 0.0f ? 0.0f : __uint_as_float(x[8 * i + 2 * k]) * f;
+                            const float b = l == 0.0f ? 0.0f : __uint_as_float(x[8 * i + 2 * k + 1]) * f;
+                            o[k] = p.bf16 ? float2_to_act2<true>(a, b) : pack_h2(a, b);
                         }
-                        __syncwarp();
+                        reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + cell * kHeadDim + 32 * c)[i] = make_uint4(o[0], o[1], o[2], o[3]);
                     }
                 }
+                __syncwarp();
             }
-        } else if (live && !part) {   // no key in sight
+        } else if (n == 0 && live && !split) {   // no key in sight
             uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + cell * kHeadDim);
             for (int i = 0; i < 16; ++i) out[i] = make_uint4(0, 0, 0, 0);
         }
-        if (live) {
-            if (part) args.part_ml[(size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell] = make_float2(m, l);
-            else if (p.lse) p.lse[cell] = log_sum(m, l);
-        }
+        if (live && split) args.part_ml[part] = make_float2(m, l);
+        else if (live && p.lse) p.lse[cell] = log_sum(m, l);
         if (!ok && lane == 0) atomicOr(p.status, WC_DEV_TIMEOUT);
         fence_before();
     } else if (warp < kMmaWarp) {
-        // keys and values: a warp looks after two pages of the tile, 8 rows of 4 chunks of 16 codes at a time: 8 lanes in
-        // a row write to distinct banks of the swizzled operand, and all addresses are a lane's own plus constants
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kConvertRegs));
+        // a warp looks after two pages of the tile; even lanes know of the first, odd ones of the second
         const int cw = warp - kSoftmaxWarps, row = lane & 7, chunk = lane >> 3;
-        const int src_at = row * kHeadDim + 16 * chunk, dst0 = (32 * cw + row) * 128 + 16 * ((2 * chunk) ^ row), dst1 = (32 * cw + row) * 128 + 16 * ((2 * chunk + 1) ^ row);
+        const int src0 = row * kHeadDim + 16 * (chunk ^ row), src1 = row * kHeadDim + 16 * ((chunk + 4) ^ row);
+        const int dst0 = (32 * cw + row) * 128 + 16 * ((2 * chunk) ^ row), dst1 = (32 * cw + row) * 128 + 16 * ((2 * chunk + 1) ^ row);
         const int32_t* table = p.block_table + (size_t)w.b * p.max_pages;
         const int pages = (w.ctx + kPage - 1) >> 4;
-        auto page_at = [&](int tile, int h) {   // -1: past the context, -2: outside the pool
-            const int page = tile * kPages + 2 * cw + h;
+        auto page_at = [&](int tile) {   // -1: past the context, -2: outside the pool
+            const int page = tile * kPages + 2 * cw + (lane & 1);
             if (tile >= t1 || page >= pages) return -1;
             const int phys = load_dep(table + page);
             return phys < 0 || phys >= p.num_pages ? -2 : phys;
         };
-        auto load = [&](const uint8_t* codes, const int (&phys)[2], uint4 (&x)[8]) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint8_t* page = codes + ((size_t)max(phys[h], 0) * p.num_kv_heads + head) * (kPage * kHeadDim) + src_at;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[4 * h + i] = make_uint4(0, 0, 0, 0);
-                    if (phys[h] >= 0) x[4 * h + i] = load_dep(reinterpret_cast<const uint4*>(page + (i >> 1) * (8 * kHeadDim) + (i & 1) * 64));
-                }
+        auto scale_at = [&](const float* scale, int phys) { return phys >= 0 && scale ? load_dep(scale + (size_t)phys * p.num_kv_heads + head) : 1.0f; };
+        auto fetch = [&](int side, int phys) {   // the warp's pages of a tile
+            const int a = __shfl_sync(0xffffffffu, phys, 0), b = __shfl_sync(0xffffffffu, phys, 1);
+            if (elect_one()) {
+                uint64_t* bar = &s.codes[side][cw];
+                uint8_t* dst = staged + side * kCodes + cw * (2 * kPage * kHeadDim);
+                mbar_arrive_expect_tx(bar, ((a >= 0) + (b >= 0)) * kPage * kHeadDim);
+                if (a >= 0) tma_page(dst, &args.maps[side], a * p.num_kv_heads + head, bar);
+                if (b >= 0) tma_page(dst + kPage * kHeadDim, &args.maps[side], b * p.num_kv_heads + head, bar);
             }
+            __syncwarp();
         };
-        auto store = [&](uint8_t* op, const uint4 (&x)[8]) {
+        // 16 codes a lane and step (8 rows of 4 chunks, conflict-free in both layouts); rows from have[h] on count as 0
+        auto expand = [&](int side, uint8_t* op, int have0, int have1) {
+            const uint8_t* src = staged + side * kCodes + cw * (2 * kPage * kHeadDim);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                uint4 x = *reinterpret_cast<const uint4*>(src + (i >> 1) * 1024 + (i & 1 ? src1 : src0));
+                if (8 * ((i >> 1) & 1) + row >= (i < 4 ? have0 : have1)) x = make_uint4(0, 0, 0, 0);
                 uint32_t h[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) codes4_to_h2<kCode>(word_of(x[i], k), h[2 * k], h[2 * k + 1]);
+                for (int k = 0; k < 4; ++k) codes4_to_h2<kCode>(word_of(x, k), h[2 * k], h[2 * k + 1]);
                 uint8_t* at = op + (i & 1) * kBlock + (i >> 1) * 1024;
                 *reinterpret_cast<uint4*>(at + dst0) = make_uint4(h[0], h[1], h[2], h[3]);
                 *reinterpret_cast<uint4*>(at + dst1) = make_uint4(h[4], h[5], h[6], h[7]);
             }
         };
         if (n > 0) {
-            int phys[2], next[2];
-            uint4 kx[8], vx[8];
-            for (int h = 0; h < 2; ++h) phys[h] = page_at(t0, h), next[h] = page_at(t0 + 1, h);
-            load(p.codes[0], phys, kx);
-            load(p.codes[1], phys, vx);
+            int phys = page_at(t0), next = page_at(t0 + 1);
+            fetch(0, phys);
+            fetch(1, phys);
+            float ks = scale_at(p.scale[0], phys), vs = scale_at(p.scale[1], phys);
             bool ok = true;
-            for (int j = 0; j < n && ok; ++j) {
+            for (int j = 0; j < n; ++j) {
                 const int st = j & 1;
                 if (j >= 2) ok = wait(s, &s.k_empty[st], ((j >> 1) - 1) & 1);
+                ok = ok && wait(s, &s.codes[0][cw], j & 1);
                 if (!ok) break;
-                bool no_values[2];
-                float vs[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const size_t at = (size_t)max(phys[h], 0) * p.num_kv_heads + head;
-                    vs[h] = phys[h] >= 0 && p.scale[1] ? load_dep(p.scale[1] + at) : 1.0f;
-                    no_values[h] = vs[h] == 0.0f;
-                    if (no_values[h]) vs[h] = 1.0f;
-                    if (lane == h) {
-                        Meta& meta = s.meta[j % kMetaStages];
-                        const float ks = phys[h] >= 0 && p.scale[0] ? load_dep(p.scale[0] + at) : 1.0f;
-                        meta.ks[2 * cw + h] = ks * p.scale_log2;
-                        meta.bias[2 * cw + h] = phys[h] == -2 ? -INFINITY : log2f(vs[h]);
-                        meta.inv[2 * cw + h] = __frcp_rn(vs[h]);
-                        if (phys[h] == -2) atomicOr(p.status, WC_DEV_BAD_PAGE);
-                    }
+                const float next_ks = scale_at(p.scale[0], next), next_vs = scale_at(p.scale[1], next);
+                // codes past the context, of no page, or of values with scale 0 must not count (NaN among them)
+                const int left = w.ctx - (t0 + j) * kTile - kPage * (2 * cw + (lane & 1)), tokens = phys < 0 ? 0 : left;
+                if (lane < 2) {
+                    Meta& meta = s.meta[j % kMetaStages];
+                    const float of = vs == 0.0f ? 1.0f : vs;
+                    meta.ks[2 * cw + lane] = ks * p.scale_log2;
+                    meta.bias[2 * cw + lane] = phys == -2 ? -INFINITY : log2f(of);
+                    meta.inv[2 * cw + lane] = __frcp_rn(of);
+                    if (phys == -2) atomicOr(p.status, WC_DEV_BAD_PAGE);
                 }
-                store(k_op + st * kOperand, kx);
+                expand(0, k_op + st * kOperand, __shfl_sync(0xffffffffu, tokens, 0), __shfl_sync(0xffffffffu, tokens, 1));
                 fence_async();
                 arrive(&s.k_full[st]);
-                load(p.codes[0], next, kx);
+                __syncwarp();
+                if (j + 1 < n) fetch(0, next);
                 if (j >= 2) ok = wait(s, &s.v_empty[st], ((j >> 1) - 1) & 1);
+                ok = ok && wait(s, &s.codes[1][cw], j & 1);
                 if (!ok) break;
-                // codes past the context, or of a page with scale 0, must not count (NaN among them)
-                const int have = w.ctx - (t0 + j) * kTile;
-                if (have < kTile || no_values[0] || no_values[1]) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (no_values[i >> 2] || 32 * cw + 8 * (i >> 1) + row >= have) vx[i] = make_uint4(0, 0, 0, 0);
-                }
-                store(v_op + st * kOperand, vx);
+                const int values = vs == 0.0f ? 0 : tokens;
+                expand(1, v_op + st * kOperand, __shfl_sync(0xffffffffu, values, 0), __shfl_sync(0xffffffffu, values, 1));
                 fence_async();
                 arrive(&s.v_full[st]);
-                load(p.codes[1], next, vx);
-                for (int h = 0; h < 2; ++h) phys[h] = next[h], next[h] = page_at(t0 + j + 2, h);
+                __syncwarp();
+                if (j + 1 < n) fetch(1, next);
+                phys = next;
+                ks = next_ks;
+                vs = next_vs;
+                next = page_at(t0 + j + 2);
             }
+            if (!ok)   // copies in flight end before the CTA does (bounded)
+                for (int side = 0; side < 2; ++side)
+                    for (int parity = 0; parity < 2; ++parity) (void)mbar_wait_bounded<64>(&s.codes[side][cw], parity);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
-        bool ok = true;
-        if (warp == kMmaWarp && n > 0 && elect_one()) {
+        if (warp == kMmaWarp && n > 0) {
+            // the warp walks together, so that operands stay in uniform registers; one lane issues
             const uint32_t q_low = operand_low(q_op, 16), k_low = operand_low(k_op, 16), v_low = operand_low(v_op, kBlock);
             auto qk = [&](int t, int st) {
                 const uint32_t q = q_low + t * (kOperand >> 4), k = k_low + st * (kOperand >> 4), d = tmem + t * kTile;
@@ -476,43 +496,46 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 }
                 commit(&s.s_full[t]);
             };
-            ok = wait(s, &s.q_full, 0) && wait(s, &s.k_full[0], 0);
+            bool ok = wait(s, &s.q_full, 0) && wait(s, &s.k_full[0], 0);
             if (ok) {
                 fence_after();
-                for (int t = 0; t < tiles_q; ++t) qk(t, 0);
-                commit(&s.k_empty[0]);
+                if (elect_one()) {
+                    qk(0, 0);
+                    if (tiles_q > 1) qk(1, 0);
+                    commit(&s.k_empty[0]);
+                }
             }
+#pragma unroll 1
             for (int j = 0; j < n && ok; ++j) {
                 const int st = j & 1;
+                const bool more = j + 1 < n;
                 ok = wait(s, &s.v_full[st], (j >> 1) & 1);
+#pragma unroll 1
                 for (int t = 0; t < tiles_q && ok; ++t) {
                     ok = wait(s, &s.p_full[t], j & 1);
+                    if (ok && more && t == 0) ok = wait(s, &s.k_full[st ^ 1], ((j + 1) >> 1) & 1);
                     if (!ok) break;
                     fence_after();
-                    const uint32_t v = v_low + st * (kOperand >> 4), pr = tmem + t * kTile, d = pr + kOutColumn;
-                    mma_ts(d, pr, operand(v), kIdescPv, j > 0);   // 16 keys each: 8 columns of P, 16 rows of V
+                    if (elect_one()) {
+                        const uint32_t v = v_low + st * (kOperand >> 4), pr = tmem + t * kTile, d = pr + kOutColumn;
+                        mma_ts(d, pr, operand(v), kIdescPv, j > 0);   // 16 keys each: 8 columns of P, 16 rows of V
 #pragma unroll
-                    for (int i = 1; i < 8; ++i) mma_ts(d, pr + 8 * i, operand(v + i * (2048 >> 4)), kIdescPv, true);
-                    if (j + 1 < n) {
-                        if (t == 0) ok = wait(s, &s.k_full[st ^ 1], ((j + 1) >> 1) & 1);
-                        if (!ok) break;
-                        fence_after();
-                        qk(t, st ^ 1);
-                    } else {
-                        commit(&s.o_full[t]);
+                        for (int i = 1; i < 8; ++i) mma_ts(d, pr + 8 * i, operand(v + i * (2048 >> 4)), kIdescPv, true);
+                        if (more) qk(t, st ^ 1);
+                        else commit(&s.o_full[t]);
+                        if (t == tiles_q - 1) {
+                            commit(&s.v_empty[st]);
+                            if (more) commit(&s.k_empty[st ^ 1]);
+                        }
                     }
-                }
-                if (ok) {
-                    commit(&s.v_empty[st]);
-                    if (j + 1 < n) commit(&s.k_empty[st ^ 1]);
+                    __syncwarp();
                 }
             }
             if (!ok) {   // what was issued ends before the accumulators are given back
-                commit(&s.drained);
+                if (elect_one()) commit(&s.drained);
                 (void)mbar_wait_bounded(&s.drained, 0);
             }
         }
-        __syncwarp();
     }
     __syncthreads();
     if (warp == kMmaWarp && n > 0) {
@@ -589,6 +612,8 @@ cudaError_t launch_block_extend(const BlockAttentionParams& p, int code, int num
     const long long cells = (long long)p.n_tok * p.num_q_heads;
     ExtendArgs args;
     args.p = p;
+    for (int side = 0; side < 2; ++side)
+        if (!encode_page_map(&args.maps[side], p.codes[side], p.num_pages, p.num_kv_heads)) return cudaErrorInvalidValue;
     args.splits = plan.splits;
     float* scratch = p.partials + block_arrived_bytes(num_sms) / sizeof(float);
     args.part_ml = reinterpret_cast<float2*>(scratch);
