@@ -46,6 +46,7 @@ struct Shared {
     uint64_t codes[2][kConvertWarps];   // a warp's two pages of keys, of values are there
     uint64_t q_full, drained, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[kTiles], p_full[kTiles], o_full[kTiles];
     Meta meta[kMetaStages];
+    float factor[kTiles * kTile];   // of a row of Q: what undoes its scaling
     uint32_t tmem;
     int abandoned;
 };
@@ -284,35 +285,50 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     if (warp < kSoftmaxWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int t = warp >> 2, thread = threadIdx.x & 127;
-        // the row's query token and head, and its output cell; not held over the loop
-        auto row_of = [&](int& token, size_t& cell) {
-            const int r = w.row0 + t * kTile + thread, i = r / p.group;
+        // a row's query token and head, and its output cell; not held over the loop
+        auto row_of = [&](int row, int& token, size_t& cell) {
+            const int r = w.row0 + row, i = (unsigned)r / (unsigned)p.group;
             token = w.lo + i;
             cell = (size_t)token * p.num_q_heads + head * p.group + r - i * p.group;
-            return t * kTile + thread < w.rows;
+            return row < w.rows;
         };
         float m = kNoMax, l = 0.0f;
         bool ok = true;
         if (n > 0) {
-            // the row of Q: bf16 scaled by a power of two into fp16's range
-            uint32_t q[64];
-            int token;
-            size_t cell;
-            const bool live = row_of(token, cell);
-            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) + (size_t)token * p.q_stride +
-                                                              (cell - (size_t)token * p.num_q_heads) * kHeadDim);
+            // Q: a half warp loads a row; bf16 rows are scaled by a power of two into fp16's range
+            const int chunk = lane & 15, row0 = t * kTile + 32 * (warp & 3);
+            uint4 x[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const uint4 x = live ? load_dep(src + i) : make_uint4(0, 0, 0, 0);
-                q[4 * i] = x.x, q[4 * i + 1] = x.y, q[4 * i + 2] = x.z, q[4 * i + 3] = x.w;
+                int token;
+                size_t cell;
+                const bool live = row_of(row0 + 2 * i + (lane >> 4), token, cell);
+                x[i] = make_uint4(0, 0, 0, 0);
+                if (live)
+                    x[i] = load_dep(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) + (size_t)token * p.q_stride +
+                                                                   (cell - (size_t)token * p.num_q_heads) * kHeadDim) + chunk);
             }
-            const float factor = p.bf16 ? bf16_row_to_f16(q, [](uint32_t x) { return x; }) : 1.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                *reinterpret_cast<uint4*>(q_op + t * kOperand + (i >> 3) * kBlock + thread * 128 + 16 * ((i & 7) ^ (thread & 7))) =
-                    make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+            for (int i = 0; i < 16; ++i) {
+                const int r = 32 * (warp & 3) + 2 * i + (lane >> 4);
+                float undo = 1.0f;
+                if (p.bf16) {
+                    uint32_t q[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                    undo = bf16_row_to_f16(q, [](uint32_t top) {
+#pragma unroll
+                        for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        return top;
+                    });
+                    x[i] = make_uint4(q[0], q[1], q[2], q[3]);
+                }
+                if (chunk == 0) s.factor[t * kTile + r] = undo;
+                *reinterpret_cast<uint4*>(q_op + t * kOperand + (chunk >> 3) * kBlock + r * 128 + 16 * ((chunk & 7) ^ (r & 7))) = x[i];
+            }
             fence_async();
             arrive(&s.q_full);
+            __syncwarp();
+            const float factor = s.factor[t * kTile + thread];
+            const bool live = t * kTile + thread < w.rows;
 
             const int seen = live ? keys_seen(p, w, w.row0 + t * kTile + thread) : 0;
             const int least = __reduce_min_sync(0xffffffffu, live ? seen : w.ctx);   // of the warp's rows
@@ -359,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         }
         int token;
         size_t cell;
-        const bool live = row_of(token, cell);
+        const bool live = row_of(t * kTile + thread, token, cell);
         const bool split = args.splits > 1;
         const size_t part = (size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell;
         if (ok && n > 0 && t < tiles_q) {
@@ -373,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         reinterpret_cast<uint4*>(args.part_o + part * kHeadDim + 32 * c)[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-                } else if (live) {
+                } else if (!split) {   // to Q's place, which the MMAs are done with
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint32_t o[4];
@@ -383,10 +399,22 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                             const float b = l == 0.0f ? 0.0f : __uint_as_float(x[8 * i + 2 * k + 1]) * f;
                             o[k] = p.bf16 ? float2_to_act2<true>(a, b) : pack_h2(a, b);
                         }
-                        reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + cell * kHeadDim + 32 * c)[i] = make_uint4(o[0], o[1], o[2], o[3]);
+                        *reinterpret_cast<uint4*>(q_op + t * kOperand + thread * 256 + 16 * ((4 * c + i) ^ (thread & 7))) = make_uint4(o[0], o[1], o[2], o[3]);
                     }
                 }
+            }
+            if (!split) {
                 __syncwarp();
+                const int chunk = lane & 15;
+#pragma unroll 4
+                for (int i = 0; i < 16; ++i) {   // whole rows, two at a time
+                    const int r = 32 * (warp & 3) + 2 * i + (lane >> 4);
+                    int to;
+                    size_t at;
+                    if (row_of(t * kTile + r, to, at))
+                        reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at * kHeadDim)[chunk] =
+                            *reinterpret_cast<const uint4*>(q_op + t * kOperand + r * 256 + 16 * (chunk ^ (r & 7)));
+                }
             }
         } else if (n == 0 && live && !split) {   // no key in sight
             uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + cell * kHeadDim);
@@ -448,7 +476,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 if (j >= 2) ok = wait(s, &s.k_empty[st], ((j >> 1) - 1) & 1);
                 ok = ok && wait(s, &s.codes[0][cw], j & 1);
                 if (!ok) break;
+                // for the next tile, and the page numbers of the one after it: a tile's time to arrive in
                 const float next_ks = scale_at(p.scale[0], next), next_vs = scale_at(p.scale[1], next);
+                const int after = page_at(t0 + j + 2);
                 // codes past the context, of no page, or of values with scale 0 must not count (NaN among them)
                 const int left = w.ctx - (t0 + j) * kTile - kPage * (2 * cw + (lane & 1)), tokens = phys < 0 ? 0 : left;
                 if (lane < 2) {
@@ -476,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 phys = next;
                 ks = next_ks;
                 vs = next_vs;
-                next = page_at(t0 + j + 2);
+                next = after;
             }
             if (!ok)   // copies in flight end before the CTA does (bounded)
                 for (int side = 0; side < 2; ++side)
