@@ -9,9 +9,9 @@
 // softmax_scale log2(e) and the row's query factor) 2^(y - m) is p vs, so O sums it times V's codes, and
 // the sum of weights takes 2^(y - m) / vs.
 // Warps 0-3 and 4-7: softmax of a tile each, a row per thread, one tile's while the tensor cores work on
-// the other's; warps 8-11: codes to fp16 operands, two stages; warp 12: the MMAs.  The codes come to
-// shared memory by TMA, two pages a warp: read with ordinary loads in rows of 64 bytes, the shape in which
-// the operands are written without bank conflicts, they cost the MMAs' operand fetch a third of its time.
+// the other's; warps 8-11: codes to fp16 operands, two stages; warp 12: the MMAs; warp 13: block table, scales
+// and the codes' way to shared memory by TMA (read with ordinary loads in rows of 64 bytes, the shape in which
+// the operands are written without bank conflicts, they cost the MMAs' operand fetch a third of its time).
 // A softmax thread moves its running maximum (and its row of O) only when a logit passes it by 2^8.
 #include "block_common.cuh"
 #include "decode_common.cuh"
@@ -24,11 +24,11 @@ constexpr int kTile = 128;                 // rows of a query tile, keys of a co
 constexpr int kPages = kTile / kPage;      // pages of a context tile
 constexpr int kTiles = 2;                  // query tiles of a CTA
 constexpr int kSoftmaxWarps = 4 * kTiles, kConvertWarps = 4;
-constexpr int kMmaWarp = kSoftmaxWarps + kConvertWarps;
+constexpr int kMmaWarp = kSoftmaxWarps + kConvertWarps, kLoadWarp = kMmaWarp + 1;
 constexpr int kThreads = 32 * (kMmaWarp + 4);
 // Registers: 128 a thread at launch, 512 threads; a softmax thread holds 64 packed weights and 32 logits and
-// takes what the MMA warps give: 256 x 176 + 128 x 96 + 128 x 64 = 512 x 128.
-constexpr int kSoftmaxRegs = 176, kConvertRegs = 96, kMmaRegs = 64;
+// takes what the MMA warps give: 256 x 176 + 128 x 80 + 128 x 80 = 512 x 128.
+constexpr int kSoftmaxRegs = 176, kConvertRegs = 80, kMmaRegs = 80;
 static_assert(kSoftmaxWarps * 32 * kSoftmaxRegs + kConvertWarps * 32 * kConvertRegs + 4 * 32 * kMmaRegs <= kThreads * 128);
 constexpr int kOperand = kTile * kHeadDim * 2;   // bytes of a [128][128] fp16 operand: two blocks of 64 channels
 constexpr int kBlock = kOperand / 2;
@@ -40,10 +40,11 @@ constexpr uint32_t kTmemColumns = 512, kOutColumn = 256;   // S (and P) of tile 
 
 struct Meta {   // of a context tile's pages
     float ks[kPages], bias[kPages], inv[kPages];
+    int tokens[2][kPages];   // rows of keys, of values that count (the others hold whatever was there, NaN codes among it)
 };
 
 struct Shared {
-    uint64_t codes[2][kConvertWarps];   // a warp's two pages of keys, of values are there
+    uint64_t codes_full[2], codes_empty[2];   // staged keys, values
     uint64_t q_full, drained, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[kTiles], p_full[kTiles], o_full[kTiles];
     Meta meta[kMetaStages];
     float factor[kTiles * kTile];   // of a row of Q: what undoes its scaling
@@ -249,8 +250,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     if (threadIdx.x == 0) {
         mbar_init(&s.q_full, kSoftmaxWarps * 32);
         mbar_init(&s.drained, 1);
-        for (int i = 0; i < 2 * kConvertWarps; ++i) mbar_init(&s.codes[0][i], 1);
         for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.codes_full[i], 1);
+            mbar_init(&s.codes_empty[i], kConvertWarps);
             mbar_init(&s.k_full[i], kConvertWarps * 32);
             mbar_init(&s.v_full[i], kConvertWarps * 32);
             mbar_init(&s.k_empty[i], 1);
@@ -426,32 +428,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         fence_before();
     } else if (warp < kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kConvertRegs));
-        // a warp looks after two pages of the tile; even lanes know of the first, odd ones of the second
-        const int cw = warp - kSoftmaxWarps, row = lane & 7, chunk = lane >> 3;
+        const int cw = warp - kSoftmaxWarps, row = lane & 7, chunk = lane >> 3;   // a warp has two pages of the tile
         const int src0 = row * kHeadDim + 16 * (chunk ^ row), src1 = row * kHeadDim + 16 * ((chunk + 4) ^ row);
         const int dst0 = (32 * cw + row) * 128 + 16 * ((2 * chunk) ^ row), dst1 = (32 * cw + row) * 128 + 16 * ((2 * chunk + 1) ^ row);
-        const int32_t* table = p.block_table + (size_t)w.b * p.max_pages;
-        const int pages = (w.ctx + kPage - 1) >> 4;
-        auto page_at = [&](int tile) {   // -1: past the context, -2: outside the pool
-            const int page = tile * kPages + 2 * cw + (lane & 1);
-            if (tile >= t1 || page >= pages) return -1;
-            const int phys = load_dep(table + page);
-            return phys < 0 || phys >= p.num_pages ? -2 : phys;
-        };
-        auto scale_at = [&](const float* scale, int phys) { return phys >= 0 && scale ? load_dep(scale + (size_t)phys * p.num_kv_heads + head) : 1.0f; };
-        auto fetch = [&](int side, int phys) {   // the warp's pages of a tile
-            const int a = __shfl_sync(0xffffffffu, phys, 0), b = __shfl_sync(0xffffffffu, phys, 1);
-            if (elect_one()) {
-                uint64_t* bar = &s.codes[side][cw];
-                uint8_t* dst = staged + side * kCodes + cw * (2 * kPage * kHeadDim);
-                mbar_arrive_expect_tx(bar, ((a >= 0) + (b >= 0)) * kPage * kHeadDim);
-                if (a >= 0) tma_page(dst, &args.maps[side], a * p.num_kv_heads + head, bar);
-                if (b >= 0) tma_page(dst + kPage * kHeadDim, &args.maps[side], b * p.num_kv_heads + head, bar);
-            }
-            __syncwarp();
-        };
-        // 16 codes a lane and step (8 rows of 4 chunks, conflict-free in both layouts); rows from have[h] on count as 0
-        auto expand = [&](int side, uint8_t* op, int have0, int have1) {
+        // 16 codes a lane and step (8 rows of 4 chunks, conflict-free in both layouts)
+        auto expand = [&](int side, uint8_t* op, const int* tokens) {
+            const int have0 = tokens[2 * cw], have1 = tokens[2 * cw + 1];
             const uint8_t* src = staged + side * kCodes + cw * (2 * kPage * kHeadDim);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -465,52 +447,22 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 *reinterpret_cast<uint4*>(at + dst1) = make_uint4(h[4], h[5], h[6], h[7]);
             }
         };
-        if (n > 0) {
-            int phys = page_at(t0), next = page_at(t0 + 1);
-            fetch(0, phys);
-            fetch(1, phys);
-            float ks = scale_at(p.scale[0], phys), vs = scale_at(p.scale[1], phys);
-            bool ok = true;
-            for (int j = 0; j < n; ++j) {
-                const int st = j & 1;
-                if (j >= 2) ok = wait(s, &s.k_empty[st], ((j >> 1) - 1) & 1);
-                ok = ok && wait(s, &s.codes[0][cw], j & 1);
+        bool ok = true;
+        for (int j = 0; j < n; ++j) {
+            const int st = j & 1;
+            const Meta& meta = s.meta[j % kMetaStages];
+#pragma unroll 1
+            for (int side = 0; side < 2 && ok; ++side) {
+                if (j >= 2) ok = wait(s, side ? &s.v_empty[st] : &s.k_empty[st], ((j >> 1) - 1) & 1);
+                ok = ok && wait(s, &s.codes_full[side], j & 1);
                 if (!ok) break;
-                // for the next tile, and the page numbers of the one after it: a tile's time to arrive in
-                const float next_ks = scale_at(p.scale[0], next), next_vs = scale_at(p.scale[1], next);
-                const int after = page_at(t0 + j + 2);
-                // codes past the context, of no page, or of values with scale 0 must not count (NaN among them)
-                const int left = w.ctx - (t0 + j) * kTile - kPage * (2 * cw + (lane & 1)), tokens = phys < 0 ? 0 : left;
-                if (lane < 2) {
-                    Meta& meta = s.meta[j % kMetaStages];
-                    const float of = vs == 0.0f ? 1.0f : vs;
-                    meta.ks[2 * cw + lane] = ks * p.scale_log2;
-                    meta.bias[2 * cw + lane] = phys == -2 ? -INFINITY : log2f(of);
-                    meta.inv[2 * cw + lane] = __frcp_rn(of);
-                    if (phys == -2) atomicOr(p.status, WC_DEV_BAD_PAGE);
-                }
-                expand(0, k_op + st * kOperand, __shfl_sync(0xffffffffu, tokens, 0), __shfl_sync(0xffffffffu, tokens, 1));
+                expand(side, (side ? v_op : k_op) + st * kOperand, meta.tokens[side]);
                 fence_async();
-                arrive(&s.k_full[st]);
+                arrive(side ? &s.v_full[st] : &s.k_full[st]);
                 __syncwarp();
-                if (j + 1 < n) fetch(0, next);
-                if (j >= 2) ok = wait(s, &s.v_empty[st], ((j >> 1) - 1) & 1);
-                ok = ok && wait(s, &s.codes[1][cw], j & 1);
-                if (!ok) break;
-                const int values = vs == 0.0f ? 0 : tokens;
-                expand(1, v_op + st * kOperand, __shfl_sync(0xffffffffu, values, 0), __shfl_sync(0xffffffffu, values, 1));
-                fence_async();
-                arrive(&s.v_full[st]);
-                __syncwarp();
-                if (j + 1 < n) fetch(1, next);
-                phys = next;
-                ks = next_ks;
-                vs = next_vs;
-                next = after;
+                if (lane == 0) arrive(&s.codes_empty[side]);
             }
-            if (!ok)   // copies in flight end before the CTA does (bounded)
-                for (int side = 0; side < 2; ++side)
-                    for (int parity = 0; parity < 2; ++parity) (void)mbar_wait_bounded<64>(&s.codes[side][cw], parity);
+            if (!ok) break;
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
@@ -565,6 +517,55 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 if (elect_one()) commit(&s.drained);
                 (void)mbar_wait_bounded(&s.drained, 0);
             }
+        } else if (warp == kLoadWarp && n > 0) {
+            // lane i < 8 looks after page i of the tile: page numbers are read two tiles ahead, scales one
+            const int page0 = t0 * kPages + lane, pages = lane < kPages ? min((w.ctx + kPage - 1) >> 4, t1 * kPages) : 0;
+            const int32_t* table = p.block_table + (size_t)w.b * p.max_pages;
+            auto number = [&](int j) { return page0 + j * kPages < pages ? load_dep(table + page0 + j * kPages) : 0; };
+            auto valid = [&](int j, int phys) { return page0 + j * kPages < pages && phys >= 0 && phys < p.num_pages; };
+            auto scale_at = [&](const float* scale, int phys, bool there) {
+                return there && scale ? load_dep(scale + (size_t)phys * p.num_kv_heads + head) : 1.0f;
+            };
+            int phys = number(0), next = number(1);
+            bool there = valid(0, phys), ok = true;
+            float ks = scale_at(p.scale[0], phys, there), vs = scale_at(p.scale[1], phys, there);
+            for (int j = 0; j < n; ++j) {
+                const bool next_there = valid(j + 1, next);
+                const float next_ks = scale_at(p.scale[0], next, next_there), next_vs = scale_at(p.scale[1], next, next_there);
+                const int after = number(j + 2);
+                const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, there)) * (kPage * kHeadDim);
+#pragma unroll
+                for (int side = 0; side < 2; ++side) {
+                    if (j > 0) ok = ok && wait(s, &s.codes_empty[side], (j - 1) & 1);
+                    if (!ok) break;
+                    if (side == 0 && lane < kPages) {   // four tiles' worth: the tile four back is done with
+                        Meta& meta = s.meta[j % kMetaStages];
+                        const bool outside = !there && page0 + j * kPages < pages;
+                        const int tokens = there ? min(kPage, w.ctx - (page0 + j * kPages) * kPage) : 0;
+                        const float of = vs == 0.0f ? 1.0f : vs;
+                        meta.ks[lane] = ks * p.scale_log2;
+                        meta.bias[lane] = outside ? -INFINITY : log2f(of);
+                        meta.inv[lane] = __frcp_rn(of);
+                        meta.tokens[0][lane] = tokens;
+                        meta.tokens[1][lane] = vs == 0.0f ? 0 : tokens;
+                        if (outside) atomicOr(p.status, WC_DEV_BAD_PAGE);
+                    }
+                    __syncwarp();
+                    if (elect_one()) mbar_arrive_expect_tx(&s.codes_full[side], bytes);
+                    __syncwarp();
+                    if (there) tma_page(staged + side * kCodes + lane * (kPage * kHeadDim), &args.maps[side], phys * p.num_kv_heads + head, &s.codes_full[side]);
+                }
+                if (!ok) break;
+                phys = next;
+                there = next_there;
+                ks = next_ks;
+                vs = next_vs;
+                next = after;
+            }
+            // copies in flight end before the CTA does (bounded): those of the last tile are all waited for by the conversion
+            if (!ok)
+                for (int side = 0; side < 2; ++side)
+                    for (int parity = 0; parity < 2; ++parity) (void)mbar_wait_bounded<64>(&s.codes_full[side], parity);
         }
     }
     __syncthreads();
