@@ -109,26 +109,20 @@ __device__ __forceinline__ void store_output(const BlockAttentionParams& p, size
     if (p.lse && lane == 0) p.lse[cell] = log_sum(m, l);
 }
 
-// N words of bf16 pairs of one row (the rest held by other lanes: across takes the maximum over
-// them) to fp16 pairs times a power of two that puts the row's largest value below 2^15: all of bf16's
-// bits stay but those below 2^-39 of the largest.  Returns the inverse factor.  Rows of zeros, infinities and NaN
-// are converted as they are.
-template <int N, typename F>
-__device__ __forceinline__ float bf16_row_to_f16(uint32_t (&w)[N], F across) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = max(top, max(w[i] << 16 & 0x7FFFFFFFu, w[i] & 0x7FFF0000u));
-    top = across(top);
+// bf16 rows as fp16: times a power of two that puts the row's largest value below 2^15, so that all of bf16's
+// bits stay but those below 2^-39 of the largest.  top: the largest of the row's words without signs, per half (as
+// integers).  Rows of zeros, infinities and NaN are converted as they are.  undo: the inverse factor.
+__device__ __forceinline__ float bf16_scale(uint32_t top, float& undo) {
+    top = max(top << 16, top & 0xFFFF0000u);
     int e = (int)(top >> 23) - 127;   // the largest is below 2^(e + 1)
     if (top == 0 || e == 128) e = 14;
     const int shift = max(min(14 - e, 126), -126);
-    const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float2 f = act2_to_float2<true>(w[i]);
-        w[i] = pack_h2(f.x * up, f.y * up);
-    }
-    return __uint_as_float((uint32_t)(127 - shift) << 23);
+    undo = __uint_as_float((uint32_t)(127 - shift) << 23);
+    return __uint_as_float((uint32_t)(127 + shift) << 23);
+}
+__device__ __forceinline__ uint32_t scaled_bf16(uint32_t w, float by) {
+    const float2 f = act2_to_float2<true>(w);
+    return pack_h2(f.x * by, f.y * by);
 }
 
 // The sequence whose first[b] is the last one <= x, for ascending first(0) <= x; a warp searches together.

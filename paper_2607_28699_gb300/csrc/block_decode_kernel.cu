@@ -182,10 +182,16 @@ __device__ __forceinline__ float load_queries(const BlockAttentionParams& p, int
 #pragma unroll
     for (int i = 0; i < 16; ++i) q[i] = word_of(w[i >> 2], i & 3);
     if (!p.bf16) return 1.0f;
-    return bf16_row_to_f16(q, [](uint32_t x) {
-        x = max(x, __shfl_xor_sync(0xffffffffu, x, 1));
-        return max(x, __shfl_xor_sync(0xffffffffu, x, 2));
-    });
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = __vmaxu2(top, q[i] & 0x7FFF7FFFu);
+    top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    float undo;
+    const float up = bf16_scale(top, undo);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) q[i] = scaled_bf16(q[i], up);
+    return undo;
 }
 
 __device__ __forceinline__ float warp_max(float x) {

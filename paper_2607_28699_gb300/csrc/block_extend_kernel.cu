@@ -47,7 +47,6 @@ struct Shared {
     uint64_t codes_full[2], codes_empty[2];   // staged keys, values
     uint64_t q_full, drained, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[kTiles], p_full[kTiles], o_full[kTiles];
     Meta meta[kMetaStages];
-    float factor[kTiles * kTile];   // of a row of Q: what undoes its scaling
     uint32_t tmem;
     int abandoned;
 };
@@ -126,6 +125,12 @@ __device__ __forceinline__ void arrive(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// 16 bytes to shared memory, of which the first `bytes` are read and the others 0.
+__device__ __forceinline__ void copy_async(void* dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // Bounded wait (about two seconds); once one gives up, all do.
 __device__ __forceinline__ bool wait(Shared& s, uint64_t* bar, uint32_t parity) {
     const uint32_t at = smem_addr(bar);
@@ -194,6 +199,23 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+
+// A tile's largest exponent alone: before a row's first tile.
+__device__ __forceinline__ float first_max(uint32_t s_at, const Meta& meta, float factor, int sees) {
+    float top = kNoMax;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        uint32_t x[32];
+        tmem_ld32(s_at + 32 * c, x);
+        tmem_wait_ld();
+        float best[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 32; i += 2)
+            best[i >> 4] = max3(best[i >> 4], 32 * c + i < sees ? __uint_as_float(x[i]) : -INFINITY, 32 * c + i + 1 < sees ? __uint_as_float(x[i + 1]) : -INFINITY);
+        top = max3(top, fmaf(best[0], meta.ks[2 * c] * factor, meta.bias[2 * c]), fmaf(best[1], meta.ks[2 * c + 1] * factor, meta.bias[2 * c + 1]));
+    }
+    return top;
 }
 
 // A row's weights for a context tile under the maximum m: pairs as fp16 in y, their sum (in units of the
@@ -287,51 +309,63 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     if (warp < kSoftmaxWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int t = warp >> 2, thread = threadIdx.x & 127;
-        // a row's query token and head, and its output cell; not held over the loop
-        auto row_of = [&](int row, int& token, size_t& cell) {
-            const int r = w.row0 + row, i = (unsigned)r / (unsigned)p.group;
-            token = w.lo + i;
-            cell = (size_t)token * p.num_q_heads + head * p.group + r - i * p.group;
-            return row < w.rows;
+        // A warp moves whole rows: a half warp a row, every second one.  The first one's token and head; two rows on.
+        const int chunk = lane & 15, warp_row = 32 * (warp & 3) + (lane >> 4);
+        struct Row {
+            int token, hq;   // hq: of the group
         };
+        auto row_at = [&](int row) {
+            const int r = w.row0 + t * kTile + row, i = (unsigned)r / (unsigned)p.group;
+            return Row{w.lo + i, r - i * p.group};
+        };
+        const int step_token = 2u / (unsigned)p.group, step_hq = 2 - step_token * p.group;
+        auto next_row = [&](Row& r) {
+            r.token += step_token;
+            r.hq += step_hq;
+            if (r.hq >= p.group) {
+                r.hq -= p.group;
+                ++r.token;
+            }
+        };
+        const int rows = w.rows - t * kTile;   // of this tile
         float m = kNoMax, l = 0.0f;
         bool ok = true;
         if (n > 0) {
-            // Q: a half warp loads a row; bf16 rows are scaled by a power of two into fp16's range
-            const int chunk = lane & 15, row0 = t * kTile + 32 * (warp & 3);
-            uint4 x[16];
-#pragma unroll
+            // Q by asynchronous copies (rows past the last: zeros); bf16 rows are then scaled by a power of two into
+            // fp16's range, a lane a row.  Short loops: this code runs once, from a cold instruction cache.
+            uint8_t* dst = q_op + t * kOperand + (chunk >> 3) * kBlock;
+            Row at = row_at(warp_row);
+#pragma unroll 2
             for (int i = 0; i < 16; ++i) {
-                int token;
-                size_t cell;
-                const bool live = row_of(row0 + 2 * i + (lane >> 4), token, cell);
-                x[i] = make_uint4(0, 0, 0, 0);
-                if (live)
-                    x[i] = load_dep(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q) + (size_t)token * p.q_stride +
-                                                                   (cell - (size_t)token * p.num_q_heads) * kHeadDim) + chunk);
+                const int r = warp_row + 2 * i;
+                const bool there = r < rows;
+                const uint16_t* src = static_cast<const uint16_t*>(p.q) + (there ? (size_t)at.token * p.q_stride + (head * p.group + at.hq) * kHeadDim + 8 * chunk : 0);
+                copy_async(dst + r * 128 + 16 * ((chunk & 7) ^ (r & 7)), src, there ? 16 : 0);
+                next_row(at);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 32 * (warp & 3) + 2 * i + (lane >> 4);
-                float undo = 1.0f;
-                if (p.bf16) {
-                    uint32_t q[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                    undo = bf16_row_to_f16(q, [](uint32_t top) {
-#pragma unroll
-                        for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        return top;
-                    });
-                    x[i] = make_uint4(q[0], q[1], q[2], q[3]);
+            copy_async_wait();
+            __syncwarp();
+            float factor = 1.0f;
+            if (p.bf16) {
+                uint8_t* row = q_op + t * kOperand + thread * 128;
+                auto word4 = [&](int i) { return reinterpret_cast<uint4*>(row + (i >> 3) * kBlock + 16 * ((i & 7) ^ (thread & 7))); };
+                uint32_t top = 0;
+#pragma unroll 8
+                for (int i = 0; i < 16; ++i) {
+                    const uint4 x = *word4(i);
+                    top = __vmaxu2(__vmaxu2(top, __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu)), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
                 }
-                if (chunk == 0) s.factor[t * kTile + r] = undo;
-                *reinterpret_cast<uint4*>(q_op + t * kOperand + (chunk >> 3) * kBlock + r * 128 + 16 * ((chunk & 7) ^ (r & 7))) = x[i];
+                const float up = bf16_scale(top, factor);
+#pragma unroll 4
+                for (int i = 0; i < 16; ++i) {
+                    uint4* at = word4(i);
+                    const uint4 x = *at;
+                    *at = make_uint4(scaled_bf16(x.x, up), scaled_bf16(x.y, up), scaled_bf16(x.z, up), scaled_bf16(x.w, up));
+                }
             }
             fence_async();
             arrive(&s.q_full);
-            __syncwarp();
-            const float factor = s.factor[t * kTile + thread];
-            const bool live = t * kTile + thread < w.rows;
-
+            const bool live = thread < rows;
             const int seen = live ? keys_seen(p, w, w.row0 + t * kTile + thread) : 0;
             const int least = __reduce_min_sync(0xffffffffu, live ? seen : w.ctx);   // of the warp's rows
             const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + t * kTile + lanes, o_at = tmem + kOutColumn + t * kTile + lanes;
@@ -345,7 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                     const bool masked = least < key0 + kTile;
                     uint32_t y[kTile / 2];
                     float sum;
-                    for (;;) {   // again where a logit passed the maximum by too much: in a row's first tile, then rarely
+                    if (j == 0) m = first_max(s_at, meta, factor, sees);
+                    for (;;) {   // again where a logit passed the maximum by too much: rarely
                         float top;
                         sum = masked ? weights<true>(s_at, meta, factor, m, sees, y, top) : weights<false>(s_at, meta, factor, m, sees, y, top);
                         if (!__any_sync(0xffffffffu, top > m + kSlack)) break;
@@ -375,10 +410,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 fence_after();
             }
         }
-        int token;
-        size_t cell;
-        const bool live = row_of(t * kTile + thread, token, cell);
-        const bool split = args.splits > 1;
+        const bool live = thread < rows, split = args.splits > 1;
+        const Row mine = row_at(thread);
+        const size_t cell = (size_t)mine.token * p.num_q_heads + head * p.group + mine.hq;
         const size_t part = (size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell;
         if (ok && n > 0 && t < tiles_q) {
             const float f = l == 0.0f ? 0.0f : __frcp_rn(l);
@@ -407,15 +441,14 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
             }
             if (!split) {
                 __syncwarp();
-                const int chunk = lane & 15;
+                Row at = row_at(warp_row);
 #pragma unroll 4
-                for (int i = 0; i < 16; ++i) {   // whole rows, two at a time
-                    const int r = 32 * (warp & 3) + 2 * i + (lane >> 4);
-                    int to;
-                    size_t at;
-                    if (row_of(t * kTile + r, to, at))
-                        reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at * kHeadDim)[chunk] =
+                for (int i = 0; i < 16; ++i) {
+                    const int r = warp_row + 2 * i;
+                    if (r < rows)
+                        reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + ((size_t)at.token * p.num_q_heads + head * p.group + at.hq) * kHeadDim)[chunk] =
                             *reinterpret_cast<const uint4*>(q_op + t * kOperand + r * 256 + 16 * (chunk ^ (r & 7)));
+                    next_row(at);
                 }
             }
         } else if (n == 0 && live && !split) {   // no key in sight
