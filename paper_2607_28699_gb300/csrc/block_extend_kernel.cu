@@ -468,13 +468,19 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         auto expand = [&](int side, uint8_t* op, const int* tokens) {
             const int have0 = tokens[2 * cw], have1 = tokens[2 * cw + 1];
             const uint8_t* src = staged + side * kCodes + cw * (2 * kPage * kHeadDim);
+            uint4 x[8];   // read first: the compiler cannot tell the stores from the loads
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const uint4*>(src + (i >> 1) * 1024 + (i & 1 ? src1 : src0));
+            if (min(have0, have1) < kPage) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (8 * ((i >> 1) & 1) + row >= (i < 4 ? have0 : have1)) x[i] = make_uint4(0, 0, 0, 0);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                uint4 x = *reinterpret_cast<const uint4*>(src + (i >> 1) * 1024 + (i & 1 ? src1 : src0));
-                if (8 * ((i >> 1) & 1) + row >= (i < 4 ? have0 : have1)) x = make_uint4(0, 0, 0, 0);
                 uint32_t h[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) codes4_to_h2<kCode>(word_of(x, k), h[2 * k], h[2 * k + 1]);
+                for (int k = 0; k < 4; ++k) codes4_to_h2<kCode>(word_of(x[i], k), h[2 * k], h[2 * k + 1]);
                 uint8_t* at = op + (i & 1) * kBlock + (i >> 1) * 1024;
                 *reinterpret_cast<uint4*>(at + dst0) = make_uint4(h[0], h[1], h[2], h[3]);
                 *reinterpret_cast<uint4*>(at + dst1) = make_uint4(h[4], h[5], h[6], h[7]);
