@@ -45,7 +45,10 @@ struct Meta {   // of a context tile's pages
 
 struct Shared {
     uint64_t codes_full[2], codes_empty[2];   // staged keys, values
-    uint64_t q_full, drained, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[kTiles], p_full[kTiles], o_full[kTiles];
+    uint64_t q_full, k_first, drained, k_empty[2], v_empty[2], s_full[kTiles], o_full[kTiles];
+    // What the MMAs of tile t and step j wait for, in one barrier (their queue is short: what the issuing warp waits, the
+    // tensor cores wait): P_t(j), V(j) and K(j + 1); by the parity of j, since the conversion runs ahead.
+    uint64_t ready[kTiles][2];
     Meta meta[kMetaStages];
     uint32_t tmem;
     int abandoned;
@@ -272,15 +275,14 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     if (threadIdx.x == 0) {
         mbar_init(&s.q_full, kSoftmaxWarps * 32);
         mbar_init(&s.drained, 1);
+        mbar_init(&s.k_first, kConvertWarps);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.codes_full[i], 1);
             mbar_init(&s.codes_empty[i], kConvertWarps);
-            mbar_init(&s.k_full[i], kConvertWarps * 32);
-            mbar_init(&s.v_full[i], kConvertWarps * 32);
             mbar_init(&s.k_empty[i], 1);
             mbar_init(&s.v_empty[i], 1);
             mbar_init(&s.s_full[i], 1);
-            mbar_init(&s.p_full[i], 128);
+            for (int k = 0; k < 2; ++k) mbar_init(&s.ready[i][k], 128 + 2 * kConvertWarps);
             mbar_init(&s.o_full[i], 1);
         }
         s.abandoned = 0;
@@ -404,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                     tmem_st32(s_at + 32, reinterpret_cast<const uint32_t(&)[32]>(y[32]));
                     tmem_wait_st();
                     fence_before();
-                    arrive(&s.p_full[t]);
+                    arrive(&s.ready[t][j & 1]);
                 }
                 ok = ok && wait(s, &s.o_full[t], 0);
                 fence_after();
@@ -497,11 +499,22 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 if (!ok) break;
                 expand(side, (side ? v_op : k_op) + st * kOperand, meta.tokens[side]);
                 fence_async();
-                arrive(side ? &s.v_full[st] : &s.k_full[st]);
                 __syncwarp();
-                if (lane == 0) arrive(&s.codes_empty[side]);
+                if (lane == 0) {
+                    arrive(&s.codes_empty[side]);
+                    if (side == 0 && j == 0) {
+                        arrive(&s.k_first);
+                    } else {   // V(j) for step j, K(j) for the step before
+                        arrive(&s.ready[0][side ? st : st ^ 1]);
+                        arrive(&s.ready[1][side ? st : st ^ 1]);
+                    }
+                }
             }
             if (!ok) break;
+        }
+        if (ok && n > 0 && lane == 0) {   // after the last step there are no keys to wait for
+            arrive(&s.ready[0][(n - 1) & 1]);
+            arrive(&s.ready[1][(n - 1) & 1]);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
@@ -517,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 }
                 commit(&s.s_full[t]);
             };
-            bool ok = wait(s, &s.q_full, 0) && wait(s, &s.k_full[0], 0);
+            bool ok = wait(s, &s.q_full, 0) && wait(s, &s.k_first, 0);
             if (ok) {
                 fence_after();
                 if (elect_one()) {
@@ -530,11 +543,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
             for (int j = 0; j < n && ok; ++j) {
                 const int st = j & 1;
                 const bool more = j + 1 < n;
-                ok = wait(s, &s.v_full[st], (j >> 1) & 1);
 #pragma unroll 1
                 for (int t = 0; t < tiles_q && ok; ++t) {
-                    ok = wait(s, &s.p_full[t], j & 1);
-                    if (ok && more && t == 0) ok = wait(s, &s.k_full[st ^ 1], ((j + 1) >> 1) & 1);
+                    ok = wait(s, &s.ready[t][st], (j >> 1) & 1);
                     if (!ok) break;
                     fence_after();
                     if (elect_one()) {
