@@ -1,4 +1,8 @@
 // Append to the block-scaled cache: rotation, page scales, 8-bit codes; queries rotated beside.
+//
+// Eight lanes hold a row, sixteen channels each: in the half layout eight pairs' lower and upper channels,
+// else sixteen neighbours, so a pair never crosses lanes and every lane's loads are 16 bytes.  A warp takes four
+// rows at a time.  Bound by memory for prompts and by latency for single tokens.
 #include "block_common.cuh"
 
 namespace wc {
@@ -6,7 +10,6 @@ namespace wc {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kQHeads = 8;   // query heads of one token that a warp rotates
 
 __device__ __forceinline__ void report(const BlockAppendParams& p, uint32_t bit) {
     if (p.dev_status) atomicOr(p.dev_status, bit);
@@ -34,55 +37,59 @@ __device__ __forceinline__ bool sequence(const BlockAppendParams& p, int b, Sequ
     return s.n > 0;
 }
 
-// A lane's eight channels 8 i .. 8 i + 7 of a row as fp32, rotated if they are among the first
-// rotary_dim: its channels and, for the half layout, their partners' come from global memory (the
-// second read hits L1), so any rotary_dim takes the same path.  Products are rounded one by
-// one: the result does not depend on what the compiler contracts.
-template <bool kBf16, bool kHalfLayout>
-__device__ __forceinline__ void load_rotated(const void* row, int i, int rot, const float* cos_row, const float* sin_row,
-                                             float (&y)[8]) {
+// Lane i of a row: its two chunks of eight channels, and whether they are rotated (i < nrot = rotary_dim / 16).
+template <bool kHalfLayout>
+struct Chunks {
+    int a, b;
+    bool rotated;
+    __device__ __forceinline__ Chunks(int i, int nrot) {
+        rotated = i < nrot;
+        a = kHalfLayout && rotated ? i : 2 * i;
+        b = kHalfLayout && rotated ? i + nrot : 2 * i + 1;
+    }
+};
+
+struct Raw {
+    uint4 a, b;
+};
+__device__ __forceinline__ Raw load_raw(const void* row, int a, int b) {
     const uint4* src = static_cast<const uint4*>(row);
-    const uint4 own = load_dep(src + i);
-    const uint32_t w[4] = {own.x, own.y, own.z, own.w};
+    return {load_dep(src + a), load_dep(src + b)};
+}
+
+// cos and sin of a lane's eight pairs.
+struct Trig {
+    float c[8], s[8];
+};
+__device__ __forceinline__ void load_trig(const BlockAppendParams& p, long long at, int i, Trig& t) {
+    const size_t off = (size_t)at * (p.rotary_dim >> 1) + 8 * i;
+    const float4* c = reinterpret_cast<const float4*>(p.cos_table + off);
+    const float4* s = reinterpret_cast<const float4*>(p.sin_table + off);
+    *reinterpret_cast<float4*>(t.c) = load_dep(c);
+    *reinterpret_cast<float4*>(t.c + 4) = load_dep(c + 1);
+    *reinterpret_cast<float4*>(t.s) = load_dep(s);
+    *reinterpret_cast<float4*>(t.s + 4) = load_dep(s + 1);
+}
+
+// A lane's sixteen channels as fp32, rotated.  Products are rounded one by one: the result does not depend on
+// what the compiler contracts.
+template <bool kBf16, bool kHalfLayout>
+__device__ __forceinline__ void rotate(const Raw& raw, bool rotated, const Trig& t, float (&y)[16]) {
+    const uint32_t w[8] = {raw.a.x, raw.a.y, raw.a.z, raw.a.w, raw.b.x, raw.b.y, raw.b.z, raw.b.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
         const float2 f = act2_to_float2<kBf16>(w[j]);
         y[2 * j] = f.x;
         y[2 * j + 1] = f.y;
     }
-    if (8 * i >= rot) return;
-    if constexpr (kHalfLayout) {
-        const int half = rot >> 4;            // 16-byte chunks of half the rotated channels
-        const bool upper = i >= half;
-        const uint4 other = load_dep(src + (upper ? i - half : i + half));
-        const uint32_t o[4] = {other.x, other.y, other.z, other.w};
-        const int j0 = 8 * (upper ? i - half : i);
-        const float4* c4 = reinterpret_cast<const float4*>(cos_row + j0);
-        const float4* s4 = reinterpret_cast<const float4*>(sin_row + j0);
-        const float4 ca = load_dep(c4), cb = load_dep(c4 + 1), sa = load_dep(s4), sb = load_dep(s4 + 1);
-        const float c[8] = {ca.x, ca.y, ca.z, ca.w, cb.x, cb.y, cb.z, cb.w};
-        const float s[8] = {sa.x, sa.y, sa.z, sa.w, sb.x, sb.y, sb.z, sb.w};
+    if (!rotated) return;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 f = act2_to_float2<kBf16>(o[j]);
-            const float ot[2] = {f.x, f.y};
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int e = 2 * j + k;
-                const float a = __fmul_rn(y[e], c[e]), b = __fmul_rn(ot[k], s[e]);
-                y[e] = upper ? __fadd_rn(a, b) : __fsub_rn(a, b);
-            }
-        }
-    } else {
-        const float4 c4 = load_dep(reinterpret_cast<const float4*>(cos_row) + i);
-        const float4 s4 = load_dep(reinterpret_cast<const float4*>(sin_row) + i);
-        const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float a = y[2 * j], b = y[2 * j + 1];
-            y[2 * j] = __fsub_rn(__fmul_rn(a, c[j]), __fmul_rn(b, s[j]));
-            y[2 * j + 1] = __fadd_rn(__fmul_rn(b, c[j]), __fmul_rn(a, s[j]));
-        }
+    for (int e = 0; e < 8; ++e) {
+        float& lo = kHalfLayout ? y[e] : y[2 * e];
+        float& hi = kHalfLayout ? y[8 + e] : y[2 * e + 1];
+        const float a = lo, b = hi;
+        lo = __fsub_rn(__fmul_rn(a, t.c[e]), __fmul_rn(b, t.s[e]));
+        hi = __fadd_rn(__fmul_rn(b, t.c[e]), __fmul_rn(a, t.s[e]));
     }
 }
 
@@ -118,12 +125,11 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
     }
 }
 
-// One warp: the new rows of one page and KV head, keys (side 0) or values.  A half warp holds
-// a row, eight channels a lane, and a lane the same channels of every second row, so the page's amax
-// is one warp reduction and the rows are read once.
+// One warp: the new rows of one page and KV head, keys (side 0) or values.  A lane holds its channels of every
+// fourth row, so the page's amax is one warp reduction and the rows are read once.
 template <int kCode, bool kBf16, bool kHalfLayout>
 __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task, int head, int side) {
-    const int lane = threadIdx.x & 31, half = lane >> 4, i = lane & 15;
+    const int lane = threadIdx.x & 31, sub = lane >> 3, i = lane & 7;
     // page tasks of sequence b: cu[b] / 16 + 2 b on, two more than its whole pages (n rows reach
     // into at most n / 16 + 2)
     int b = task, local = 0;
@@ -147,94 +153,114 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
     const uint32_t had = keep ? __float_as_uint(load_dep(p.scale[side] + block)) : 0u;
     const int rot = side == 0 ? p.rotary_dim : 0;
 
-    float y[kPage / 2][8];
-    bool mine[kPage / 2];
-    uint32_t amax = 0;
-    const char* rows = static_cast<const char*>(p.x[side]);
+    const Chunks<kHalfLayout> at(i, rot >> 4);
+    constexpr int kSteps = kPage / 4;
+    Raw raw[kSteps];
+    long long position[kSteps];
+    bool mine[kSteps];
+    const char* rows = static_cast<const char*>(p.x[side]) + 2 * ((size_t)head * kHeadDim);
 #pragma unroll
-    for (int j = 0; j < kPage / 2; ++j) {
-        const int t = page * kPage + 2 * j + half;
+    for (int j = 0; j < kSteps; ++j) {
+        const int t = page * kPage + 4 * j + sub;
         mine[j] = t >= t0 && t < t1;
         const int row = s.lo + t - s.start;
-        long long at = 0;
-        if (rot && mine[j]) {
-            at = p.positions ? load_dep(p.positions + row) : t;
-            if (at < 0 || at >= p.num_positions) {
-                report(p, WC_DEV_BAD_POSITION);
-                mine[j] = false;
-            }
+        raw[j] = {};
+        position[j] = t;
+        if (mine[j]) {
+            raw[j] = load_raw(rows + 2 * ((size_t)row * p.x_stride[side]), at.a, at.b);
+            if (rot && p.positions) position[j] = load_dep(p.positions + row);
+        }
+    }
+    float y[kSteps][16];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        if (rot && mine[j] && (position[j] < 0 || position[j] >= p.num_positions)) {
+            report(p, WC_DEV_BAD_POSITION);
+            mine[j] = false;
         }
         if (mine[j]) {
-            const size_t trig = (size_t)at * (rot >> 1);
-            load_rotated<kBf16, kHalfLayout>(rows + 2 * ((size_t)row * p.x_stride[side] + (size_t)head * kHeadDim), i, rot,
-                                             p.cos_table + trig, p.sin_table + trig, y[j]);
+            Trig trig;
+            if (at.rotated) load_trig(p, position[j], i, trig);
+            rotate<kBf16, kHalfLayout>(raw[j], at.rotated, trig, y[j]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(y[j][e]) & 0x7FFFFFFFu);
+            for (int e = 0; e < 16; ++e) amax = max(amax, __float_as_uint(y[j][e]) & 0x7FFFFFFFu);
         }
     }
     amax = __reduce_max_sync(0xffffffffu, amax);
     const uint32_t now = max(scale_bits<kCode>(amax), had);
     const bool finite = now < 0x7F800000u;
     const float scale = __uint_as_float(now), inv = now && finite ? __fdiv_rn(1.0f, scale) : 0.0f;
-    uint8_t* codes = p.codes[side] + block * (kPage * kHeadDim) + 8 * i;
+    uint8_t* codes = p.codes[side] + block * (kPage * kHeadDim);
 #pragma unroll
-    for (int j = 0; j < kPage / 2; ++j) {
+    for (int j = 0; j < kSteps; ++j) {
         if (!mine[j]) continue;
-        float v[8];
+        float v[16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = finite ? __fmul_rn(y[j][e], inv) : 0.0f;
-        *reinterpret_cast<uint2*>(codes + (2 * j + half) * kHeadDim) =
-            make_uint2(encode4<kCode>(v[0], v[1], v[2], v[3]), encode4<kCode>(v[4], v[5], v[6], v[7]));
+        for (int e = 0; e < 16; ++e) v[e] = finite ? __fmul_rn(y[j][e], inv) : 0.0f;
+        uint2* dst = reinterpret_cast<uint2*>(codes + (4 * j + sub) * kHeadDim);
+        dst[at.a] = make_uint2(encode4<kCode>(v[0], v[1], v[2], v[3]), encode4<kCode>(v[4], v[5], v[6], v[7]));
+        dst[at.b] = make_uint2(encode4<kCode>(v[8], v[9], v[10], v[11]), encode4<kCode>(v[12], v[13], v[14], v[15]));
     }
     if (now > had) {
         if (lane == 0) p.scale[side][block] = scale;
         const float ratio = finite ? __fdiv_rn(__uint_as_float(had), scale) : 0.0f;
-        for (int r = half; r < keep; r += 2) {   // older tokens: the page's scale grew
-            uint2* at = reinterpret_cast<uint2*>(codes + r * kHeadDim);
-            const uint2 c = load_dep(at);
-            uint32_t h[4];
-            codes4_to_h2<kCode>(c.x, h[0], h[1]);
-            codes4_to_h2<kCode>(c.y, h[2], h[3]);
-            float v[8];
+        for (int r = sub; r < keep; r += 4) {   // older tokens: the page's scale grew
+            uint4* old = reinterpret_cast<uint4*>(codes + r * kHeadDim) + i;
+            const uint4 c = load_dep(old);
+            uint32_t out[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 f = h2_to_float2(h[e]);
-                v[2 * e] = finite ? __fmul_rn(f.x, ratio) : 0.0f;
-                v[2 * e + 1] = finite ? __fmul_rn(f.y, ratio) : 0.0f;
+            for (int k = 0; k < 4; ++k) {
+                uint32_t lo, hi;
+                codes4_to_h2<kCode>(word_at(c, k), lo, hi);
+                const float2 f = h2_to_float2(lo), g = h2_to_float2(hi);
+                out[k] = finite ? encode4<kCode>(__fmul_rn(f.x, ratio), __fmul_rn(f.y, ratio), __fmul_rn(g.x, ratio), __fmul_rn(g.y, ratio)) : 0u;
             }
-            *at = make_uint2(encode4<kCode>(v[0], v[1], v[2], v[3]), encode4<kCode>(v[4], v[5], v[6], v[7]));
+            *old = make_uint4(out[0], out[1], out[2], out[3]);
         }
     } else if (!keep && lane == 0) {
         p.scale[side][block] = scale;   // a page begun with zeros
     }
 }
 
-// One warp: kQHeads query heads of one token.
+// One warp: query heads [head0, head0 + p.q_heads) of one token.
 template <bool kBf16, bool kHalfLayout>
 __device__ __forceinline__ void rotate_queries(const BlockAppendParams& p, int row, int head0) {
-    const int lane = threadIdx.x & 31, half = lane >> 4, i = lane & 15;
-    const int rot = p.rotary_dim;
-    long long at = 0;
+    const int lane = threadIdx.x & 31, sub = lane >> 3, i = lane & 7;
+    const int rot = p.rotary_dim, end = min(head0 + p.q_heads, p.num_q_heads);
+    const Chunks<kHalfLayout> at(i, rot >> 4);
+    const char* src = static_cast<const char*>(p.q) + 2 * (size_t)row * p.q_stride;
+    char* dst = static_cast<char*>(p.q_out) + 2 * (size_t)row * p.num_q_heads * kHeadDim;
     int b = row;
     if (p.cu_new) b = warp_find_last(p.batch, row, [&](int s) { return (long long)load_dep(p.cu_new + s); });
     Sequence s;
-    if (!sequence(p, b, s) || row < s.lo || row >= s.lo + s.n) return;
-    if (rot) at = p.positions ? load_dep(p.positions + row) : s.start + row - s.lo;
-    const bool bad = rot && (at < 0 || at >= p.num_positions);
+    if (!sequence(p, b, s) || row < s.lo || row >= s.lo + s.n) return;   // reported elsewhere
+    long long position = s.start + row - s.lo;
+    if (rot && p.positions) position = load_dep(p.positions + row);
+    const bool bad = rot && (position < 0 || position >= p.num_positions);
     if (bad && lane == 0) report(p, WC_DEV_BAD_POSITION);
-    const size_t trig = (size_t)(bad ? 0 : at) * (rot >> 1);
-    const char* src = static_cast<const char*>(p.q) + 2 * (size_t)row * p.q_stride;
-    char* dst = static_cast<char*>(p.q_out) + 2 * (size_t)row * p.num_q_heads * kHeadDim;
+    Trig trig;
+    if (at.rotated && !bad) load_trig(p, position, i, trig);
+    constexpr int kAhead = 4;   // steps of four heads in flight
+    for (int h0 = head0 + sub; h0 - sub < end; h0 += 4 * kAhead) {
+        Raw raw[kAhead];
 #pragma unroll
-    for (int j = 0; j < kQHeads / 2; ++j) {
-        const int h = head0 + 2 * j + half;
-        if (h >= p.num_q_heads) continue;
-        float y[8] = {};
-        if (!bad)
-            load_rotated<kBf16, kHalfLayout>(src + 2 * (size_t)h * kHeadDim, i, rot, p.cos_table + trig, p.sin_table + trig, y);
-        reinterpret_cast<uint4*>(dst + 2 * (size_t)h * kHeadDim)[i] =
-            make_uint4(float2_to_act2<kBf16>(y[0], y[1]), float2_to_act2<kBf16>(y[2], y[3]), float2_to_act2<kBf16>(y[4], y[5]),
-                       float2_to_act2<kBf16>(y[6], y[7]));
+        for (int j = 0; j < kAhead; ++j) {
+            raw[j] = {};
+            if (h0 + 4 * j < end && !bad) raw[j] = load_raw(src + 2 * (size_t)(h0 + 4 * j) * kHeadDim, at.a, at.b);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (h0 + 4 * j >= end) continue;
+            float y[16];
+            rotate<kBf16, kHalfLayout>(raw[j], at.rotated && !bad, trig, y);
+            uint4* out = reinterpret_cast<uint4*>(dst + 2 * (size_t)(h0 + 4 * j) * kHeadDim);
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = float2_to_act2<kBf16>(y[2 * e], y[2 * e + 1]);
+            out[at.a] = make_uint4(w[0], w[1], w[2], w[3]);
+            out[at.b] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
     }
 }
 
@@ -256,10 +282,10 @@ __global__ void __launch_bounds__(kThreads) block_append_kernel(const __grid_con
         append_page<kCode, kBf16, kHalfLayout>(p, (int)task, rest >> 1, rest & 1);
     } else {
         const long long t = (long long)(blockIdx.x - p.page_ctas) * kWarps + warp;
-        const int per = (p.num_q_heads + kQHeads - 1) / kQHeads;
+        const int per = (p.num_q_heads + p.q_heads - 1) / p.q_heads;
         const long long row = t / per;
         if (row >= p.n_tok) return;
-        rotate_queries<kBf16, kHalfLayout>(p, (int)row, (int)(t - row * per) * kQHeads);
+        rotate_queries<kBf16, kHalfLayout>(p, (int)row, (int)(t - row * per) * p.q_heads);
     }
 }
 
@@ -269,7 +295,9 @@ cudaError_t launch_block_append(const BlockAppendParams& params, int code, int a
     BlockAppendParams p = params;
     const long long pages = p.cu_new ? (long long)p.n_tok / kPage + 2LL * p.batch : p.batch;
     const long long page_ctas = (pages * 2 * p.num_kv_heads + 1 + kWarps - 1) / kWarps;
-    const long long q_ctas = p.q ? ((long long)p.n_tok * ((p.num_q_heads + kQHeads - 1) / kQHeads) + kWarps - 1) / kWarps : 0;
+    // few tokens: eight heads a warp, in parallel; many: sixteen, behind one read of the angles
+    p.q_heads = (long long)p.n_tok * p.num_q_heads >= 16384 ? 16 : 8;
+    const long long q_ctas = p.q ? ((long long)p.n_tok * ((p.num_q_heads + p.q_heads - 1) / p.q_heads) + kWarps - 1) / kWarps : 0;
     if (page_ctas + q_ctas > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
     p.page_tasks = (int)pages;
     p.page_ctas = (int)page_ctas;

@@ -27,6 +27,7 @@ struct BlockAppendParams {
     int32_t n_tok, batch, max_pages, num_pages, num_q_heads, num_kv_heads, num_positions, rotary_dim;
     int32_t page_tasks;        // upper bound of the pages written, over all sequences
     int32_t page_ctas;         // CTAs of the page tasks; those after them rotate queries
+    int32_t q_heads;           // query heads of one token that a warp takes
 };
 
 struct BlockAttentionParams {
@@ -77,6 +78,8 @@ __device__ __forceinline__ uint32_t float2_to_act2(float lo, float hi) {
         return pack_h2(lo, hi);
     }
 }
+
+__device__ __forceinline__ uint32_t word_at(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // Four codes of a word as two exact half2 (codes 0, 1 and 2, 3).
 template <int kCode>
