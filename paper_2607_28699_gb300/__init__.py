@@ -497,7 +497,7 @@ class BlockDesc:
                           self.code, self.rope_layout, self.rotary_dim)
 
 
-@dataclass
+@dataclass(frozen=True)
 class BlockCache:
     """One layer's block-scaled cache tensors (layout in ``include/witcert.h``); without scales
     (None) a cache of raw fp8 codes, such as a ``LayerCache``'s of the fp8 scheme."""
@@ -505,6 +505,16 @@ class BlockCache:
     v_codes: torch.Tensor
     k_scale: Optional[torch.Tensor]
     v_scale: Optional[torch.Tensor]
+
+    def __post_init__(self):
+        blocks = self.k_codes.numel() // (16 * 128)      # pages x KV heads
+        for t in (self.k_codes, self.v_codes):
+            if t.element_size() != 1 or t.numel() != blocks * 16 * 128 or not t.is_contiguous():
+                raise ValueError("the cache's codes must be contiguous bytes [num_pages, num_kv_heads, 16, 128]")
+        for t in (self.k_scale, self.v_scale):
+            if t is not None and (t.dtype != torch.float32 or t.numel() != blocks or not t.is_contiguous()):
+                raise ValueError("the cache's scales must be contiguous float32 [num_pages, num_kv_heads]")
+        object.__setattr__(self, "blocks", blocks)
 
     @staticmethod
     def empty(desc: BlockDesc, device="cuda"):
@@ -539,44 +549,32 @@ class BlockWorkspace:
 _ACT = {torch.float16: ACT_FP16, torch.bfloat16: ACT_BF16}
 
 
-def _act(t: torch.Tensor):
-    a = _ACT.get(t.dtype)
-    if a is None:
-        raise ValueError(f"expected a float16 or bfloat16 tensor, got {t.dtype}")
-    return a
-
-
-def _rows(t: torch.Tensor, heads: int, act: int, name: str):
-    """Pointer and token stride of [n, heads, 128] rows whose heads are contiguous (a view of a
-    packed projection, for instance)."""
-    shape = t.shape
-    if len(shape) != 3 or shape[1] != heads or shape[2] != 128:
-        raise ValueError(f"{name} must be [n, {heads}, 128], got {list(shape)}")
-    if _ACT.get(t.dtype) != act:
-        raise ValueError(f"{name} has another element type: {t.dtype}")
-    s = t.stride()
-    if s[2] != 1 or (s[1] != 128 and heads > 1):
+# As above, a short call is bound by this marshalling (an append of one token: 5 us on the GPU), so the checks
+# are few and in line.
+def _rows(t: torch.Tensor, heads: int, act, name: str):
+    """Token stride of [n, heads, 128] rows whose heads are contiguous (a view of a packed projection, for
+    instance)."""
+    n, h, d = t.shape
+    if h != heads or d != 128 or _ACT.get(t.dtype) != act or act is None:
+        raise ValueError(f"{name} must be float16 or bfloat16 [n, {heads}, 128] like the others, got {t.dtype} {list(t.shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (s1 != 128 and heads > 1):
         raise ValueError(f"{name}'s heads must be contiguous")
-    return t.data_ptr(), s[0] if shape[0] > 1 else max(s[0], heads * 128)
+    return s0 if n > 1 else heads * 128
 
 
-def _ints(t: Optional[torch.Tensor], n: int, name: str):
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or t.numel() != n:
-        raise ValueError(f"{name} must hold {n} int32 values, got {t.numel()} {t.dtype}")
-    return _ptr(t)
+def _ints(t: torch.Tensor, n: int, name: str):
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and hold {n} int32 values, got {t.numel()} {t.dtype}")
+    return t.data_ptr()
 
 
-def _block_cache(desc: BlockDesc, cache: BlockCache):
-    n = desc.num_pages * desc.num_kv_heads
-    for t in (cache.k_codes, cache.v_codes):
-        if t.element_size() != 1 or t.numel() != n * desc.page_size * desc.head_dim:
-            raise ValueError("the cache's codes do not have the descriptor's shape")
-    for t in (cache.k_scale, cache.v_scale):
-        if t is not None and (t.dtype != torch.float32 or t.numel() != n):
-            raise ValueError("the cache's scales must be float32 [num_pages, num_kv_heads]")
-    return _ptr(cache.k_codes), _ptr(cache.v_codes), _ptr(cache.k_scale), _ptr(cache.v_scale)
+def _block_cache(desc: BlockDesc, c: BlockCache):
+    if c.blocks != desc.num_pages * desc.num_kv_heads:
+        raise ValueError("the cache does not have the descriptor's shape")
+    ks, vs = c.k_scale, c.v_scale
+    return (c.k_codes.data_ptr(), c.v_codes.data_ptr(), None if ks is None else ks.data_ptr(),
+            None if vs is None else vs.data_ptr())
 
 
 def block_append(desc: BlockDesc, k: torch.Tensor, v: torch.Tensor, ctx_lens: torch.Tensor, block_table: torch.Tensor,
@@ -588,44 +586,55 @@ def block_append(desc: BlockDesc, k: torch.Tensor, v: torch.Tensor, ctx_lens: to
     contexts of ctx_lens int32 [B]; cu_new int32 [B + 1], None: one token per sequence; cos, sin fp32
     [positions, rotary_dim / 2].  Returns the rotated queries (``q_out``) if ``q`` [n_tok, Hq, 128] is given."""
     batch, max_pages = block_table.shape
-    act, n_tok = _act(k), k.shape[0]
-    kp, ks = _rows(k, desc.num_kv_heads, act, "k")
-    vp, vs = _rows(v, desc.num_kv_heads, act, "v")
-    if v.shape[0] != n_tok or (q is not None and q.shape[0] != n_tok):
-        raise ValueError("k, v and q must have the same number of tokens")
-    qp, qs = None, 0
+    act, n_tok, hkv = _ACT.get(k.dtype), k.shape[0], desc.num_kv_heads
+    ks, vs = _rows(k, hkv, act, "k"), _rows(v, hkv, act, "v")
+    if v.shape[0] != n_tok:
+        raise ValueError("k and v must have the same number of tokens")
+    qp = op = None
+    qs = num_positions = 0
     if q is not None:
-        qp, qs = _rows(q, desc.num_q_heads, act, "q")
+        qs = _rows(q, desc.num_q_heads, act, "q")
+        if q.shape[0] != n_tok:
+            raise ValueError("k and q must have the same number of tokens")
         if q_out is None:
-            q_out = torch.empty(n_tok, desc.num_q_heads, 128, dtype=q.dtype, device=q.device)
-        elif q_out.shape != q.shape or q_out.dtype != q.dtype:
-            raise ValueError("q_out must have q's shape and type")
-    num_positions = 0
+            q_out = q.new_empty((n_tok, desc.num_q_heads, 128))
+        elif q_out.shape != q.shape or q_out.dtype != q.dtype or not q_out.is_contiguous():
+            raise ValueError("q_out must be contiguous and have q's shape and type")
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    cp = sp = None
     if cos is not None:
-        num_positions = cos.shape[0]
-        for t in (cos, sin):
-            if t is None or t.dtype != torch.float32 or tuple(t.shape) != (num_positions, desc.rotary_dim // 2):
-                raise ValueError(f"cos and sin must be float32 [positions, {desc.rotary_dim // 2}]")
+        shape = cos.shape
+        if (sin is None or sin.shape != shape or len(shape) != 2 or shape[1] * 2 != desc.rotary_dim or cos.dtype != torch.float32
+                or sin.dtype != torch.float32 or not cos.is_contiguous() or not sin.is_contiguous()):
+            raise ValueError(f"cos and sin must be contiguous float32 [positions, {desc.rotary_dim // 2}]")
+        num_positions, cp, sp = shape[0], cos.data_ptr(), sin.data_ptr()
     d = desc.c()
-    _check(lib.wc_block_append(
-        ctypes.byref(d), act, kp, ks, vp, vs, qp, qs, _ptr(q_out), n_tok, _ints(cu_new, batch + 1, "cu_new"),
-        _ints(block_table, batch * max_pages, "block_table"), max_pages, _ints(ctx_lens, batch, "ctx_lens"), batch,
-        _ints(positions, n_tok, "positions"), _ptr(cos), _ptr(sin), num_positions, *_block_cache(desc, cache),
-        _ptr(dev_status), _stream(stream)))
+    st = lib.wc_block_append(
+        ctypes.byref(d), act, k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, n_tok,
+        None if cu_new is None else _ints(cu_new, batch + 1, "cu_new"), _ints(block_table, batch * max_pages, "block_table"),
+        max_pages, _ints(ctx_lens, batch, "ctx_lens"), batch,
+        None if positions is None else _ints(positions, n_tok, "positions"), cp, sp, num_positions,
+        *_block_cache(desc, cache), _ptr(dev_status), _stream(stream))
+    if st:
+        _check(st)
     return q_out
 
 
 def _attention_out(desc, q, out, lse, return_lse):
     n_tok = q.shape[0]
     if out is None:
-        out = torch.empty(n_tok, desc.num_q_heads, 128, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out must have q's shape and type")
+        out = q.new_empty((n_tok, desc.num_q_heads, 128))
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be contiguous and have q's shape and type")
     if lse is None:
-        lse = torch.empty(n_tok, desc.num_q_heads, dtype=torch.float32, device=q.device) if return_lse else None
-    elif lse.dtype != torch.float32 or lse.numel() != n_tok * desc.num_q_heads:
-        raise ValueError("lse must be float32 [n_tok, num_q_heads]")
+        if return_lse:
+            lse = torch.empty(n_tok, desc.num_q_heads, dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.numel() != n_tok * desc.num_q_heads or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous float32 [n_tok, num_q_heads]")
     return out, lse
+
+
+_SCALE_128 = 1.0 / math.sqrt(128)
 
 
 def block_decode_attention(desc: BlockDesc, q: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
@@ -634,17 +643,19 @@ def block_decode_attention(desc: BlockDesc, q: torch.Tensor, block_table: torch.
     """``wc_block_decode_attention``: q [B, Hq, 128], one token per sequence; softmax_scale 1 / sqrt(128) unless given.
     Returns out, or (out, lse) with ``return_lse`` or an ``lse`` to fill."""
     batch, max_pages = block_table.shape
-    act = _act(q)
-    qp, qs = _rows(q, desc.num_q_heads, act, "q")
+    act = _ACT.get(q.dtype)
+    qs = _rows(q, desc.num_q_heads, act, "q")
     if q.shape[0] != batch:
         raise ValueError(f"q must have one token per sequence ({batch}), got {q.shape[0]}")
     out, lse = _attention_out(desc, q, out, lse, return_lse)
     d = desc.c()
-    _check(lib.wc_block_decode_attention(
-        ctypes.byref(d), act, qp, qs, _ints(block_table, batch * max_pages, "block_table"), max_pages,
+    st = lib.wc_block_decode_attention(
+        ctypes.byref(d), act, q.data_ptr(), qs, _ints(block_table, batch * max_pages, "block_table"), max_pages,
         _ints(ctx_lens, batch, "ctx_lens"), batch, *_block_cache(desc, cache),
-        1.0 / math.sqrt(128) if softmax_scale is None else softmax_scale, _ptr(out), _ptr(lse), ws.view.data_ptr(),
-        ws.nbytes, _stream(stream)))
+        _SCALE_128 if softmax_scale is None else softmax_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+        ws.view.data_ptr(), ws.nbytes, _stream(stream))
+    if st:
+        _check(st)
     return out if lse is None else (out, lse)
 
 
@@ -655,15 +666,17 @@ def block_extend_attention(desc: BlockDesc, q: torch.Tensor, cu_q: torch.Tensor,
     """``wc_block_extend_attention``: q [n_tok, Hq, 128], rows cu_q[b] .. cu_q[b + 1] - 1 the last tokens of sequence
     b's context.  Returns out, or (out, lse) with ``return_lse`` or an ``lse`` to fill."""
     batch, max_pages = block_table.shape
-    act = _act(q)
-    qp, qs = _rows(q, desc.num_q_heads, act, "q")
+    act = _ACT.get(q.dtype)
+    qs = _rows(q, desc.num_q_heads, act, "q")
     out, lse = _attention_out(desc, q, out, lse, return_lse)
     d = desc.c()
-    _check(lib.wc_block_extend_attention(
-        ctypes.byref(d), act, qp, qs, q.shape[0], _ints(cu_q, batch + 1, "cu_q"),
+    st = lib.wc_block_extend_attention(
+        ctypes.byref(d), act, q.data_ptr(), qs, q.shape[0], _ints(cu_q, batch + 1, "cu_q"),
         _ints(block_table, batch * max_pages, "block_table"), max_pages, _ints(ctx_lens, batch, "ctx_lens"), batch,
-        *_block_cache(desc, cache), 1.0 / math.sqrt(128) if softmax_scale is None else softmax_scale, int(causal),
-        _ptr(out), _ptr(lse), ws.view.data_ptr(), ws.nbytes, _stream(stream)))
+        *_block_cache(desc, cache), _SCALE_128 if softmax_scale is None else softmax_scale, int(causal),
+        out.data_ptr(), None if lse is None else lse.data_ptr(), ws.view.data_ptr(), ws.nbytes, _stream(stream))
+    if st:
+        _check(st)
     return out if lse is None else (out, lse)
 
 

@@ -171,7 +171,13 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
             if (rot && p.positions) position[j] = load_dep(p.positions + row);
         }
     }
-    float y[kSteps][16];
+    // Rows are rotated for their amax and again for their codes: kept as fp32 they would take the registers of a
+    // third of the warps.
+    auto turned = [&](int j, float (&y)[16]) {
+        Trig trig;
+        if (at.rotated) load_trig(p, position[j], i, trig);
+        rotate<kBf16, kHalfLayout>(raw[j], at.rotated, trig, y);
+    };
     uint32_t amax = 0;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
@@ -180,11 +186,10 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
             mine[j] = false;
         }
         if (mine[j]) {
-            Trig trig;
-            if (at.rotated) load_trig(p, position[j], i, trig);
-            rotate<kBf16, kHalfLayout>(raw[j], at.rotated, trig, y[j]);
+            float y[16];
+            turned(j, y);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) amax = max(amax, __float_as_uint(y[j][e]) & 0x7FFFFFFFu);
+            for (int e = 0; e < 16; ++e) amax = max(amax, __float_as_uint(y[e]) & 0x7FFFFFFFu);
         }
     }
     amax = __reduce_max_sync(0xffffffffu, amax);
@@ -196,8 +201,9 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
     for (int j = 0; j < kSteps; ++j) {
         if (!mine[j]) continue;
         float v[16];
+        turned(j, v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = finite ? __fmul_rn(y[j][e], inv) : 0.0f;
+        for (int e = 0; e < 16; ++e) v[e] = finite ? __fmul_rn(v[e], inv) : 0.0f;
         uint2* dst = reinterpret_cast<uint2*>(codes + (4 * j + sub) * kHeadDim);
         dst[at.a] = make_uint2(encode4<kCode>(v[0], v[1], v[2], v[3]), encode4<kCode>(v[4], v[5], v[6], v[7]));
         dst[at.b] = make_uint2(encode4<kCode>(v[8], v[9], v[10], v[11]), encode4<kCode>(v[12], v[13], v[14], v[15]));
@@ -265,7 +271,7 @@ __device__ __forceinline__ void rotate_queries(const BlockAppendParams& p, int r
 }
 
 template <int kCode, bool kBf16, bool kHalfLayout>
-__global__ void __launch_bounds__(kThreads) block_append_kernel(const __grid_constant__ BlockAppendParams p) {
+__global__ void __launch_bounds__(kThreads, 3) block_append_kernel(const __grid_constant__ BlockAppendParams p) {
     grid_dep_launch();
     grid_dep_wait();
     const int warp = threadIdx.x >> 5;
@@ -295,8 +301,8 @@ cudaError_t launch_block_append(const BlockAppendParams& params, int code, int a
     BlockAppendParams p = params;
     const long long pages = p.cu_new ? (long long)p.n_tok / kPage + 2LL * p.batch : p.batch;
     const long long page_ctas = (pages * 2 * p.num_kv_heads + 1 + kWarps - 1) / kWarps;
-    // few tokens: eight heads a warp, in parallel; many: sixteen, behind one read of the angles
-    p.q_heads = (long long)p.n_tok * p.num_q_heads >= 16384 ? 16 : 8;
+    // few tokens: eight heads a warp, in parallel; many: 32, behind one read of the angles
+    p.q_heads = (long long)p.n_tok * p.num_q_heads >= 16384 ? 32 : 8;
     const long long q_ctas = p.q ? ((long long)p.n_tok * ((p.num_q_heads + p.q_heads - 1) / p.q_heads) + kWarps - 1) / kWarps : 0;
     if (page_ctas + q_ctas > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
     p.page_tasks = (int)pages;

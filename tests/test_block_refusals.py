@@ -117,10 +117,13 @@ def test_binding_checks_tensors(wc):
     for k2, v2, kw in ((k.float(), k, {}), (k, k.bfloat16(), {}), (k[:, :1], k, {}), (k, k[:4], {}), (k, k[..., ::2], {}),
                        (k, k, {"ctx_lens": torch.tensor([3, 2])}), (k, k, {"cu_new": i32(0, 5)}), (k, k, {"cos": torch.zeros(8, 32)}),
                        (k, k, {"sin": None}), (k, k, {"positions": i32(0)}), (k, k, {"q": torch.zeros(5, 2, 128, dtype=torch.float16)}),
-                       (k, k, {"cache": wc.BlockCache(c.k_codes[:2], c.v_codes, c.k_scale, c.v_scale)}),
-                       (k, k, {"cache": wc.BlockCache(c.k_codes, c.v_codes, c.k_scale.half(), c.v_scale)})):
+                       (k, k, {"cache": wc.BlockCache.empty(wc.BlockDesc(num_q_heads=4, num_kv_heads=2, num_pages=2), device="cpu")})):
         with pytest.raises(ValueError):
             wc.block_append(d, k2, v2, **{**ok, **kw}, stream=torch.Stream("cpu"))
+    for bad in ((c.k_codes[:2], c.v_codes, c.k_scale, c.v_scale), (c.k_codes, c.v_codes, c.k_scale.half(), c.v_scale),
+                (c.k_codes.half(), c.v_codes, c.k_scale, c.v_scale), (c.k_codes, c.v_codes.transpose(2, 3), None, None)):
+        with pytest.raises(ValueError):
+            wc.BlockCache(*bad)
     q = torch.zeros(2, 4, 128, dtype=torch.float16)
     for q2, kw in ((q.float(), {}), (q[:1], {}), (q, {"out": q[:1]}), (q, {"lse": torch.zeros(3)}), (q[:, :2], {})):
         with pytest.raises(ValueError):
