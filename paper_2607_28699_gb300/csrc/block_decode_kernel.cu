@@ -136,35 +136,42 @@ __device__ __forceinline__ int sequence_at(const Shared& s, int batch, int r) {
     return lo;
 }
 
-// What a lane knows of one page of its warp's range.
+// What a lane knows of one page of its warp's range.  Found in two steps, so that no step waits for a load that it
+// has just issued: where the page is in the block table, then (page_resolve) its scales.
 struct PageEntry {
-    int row;       // first row of the code arrays' (page, head) index
+    int row;       // page number, then (page, head) index of the code arrays
     int unit;      // Unit::id
     int info;      // tokens to read | kFirst | kLast
     float ks, vs;  // key scale, value scale
 };
 constexpr int kTokens = 31, kFirst = 32, kLast = 64;
 
-__device__ __forceinline__ PageEntry page_entry(const BlockAttentionParams& p, const Shared& s, int head0, int per_head, int at, int first, int last) {
-    PageEntry e = {0, 0, 0, 0.0f, 1.0f};
+__device__ __forceinline__ PageEntry page_find(const BlockAttentionParams& p, const Shared& s, int head0, int per_head, int at, int first, int last) {
+    PageEntry e = {0, head0 << kSequenceBits, 0, 0.0f, 1.0f};
     if (at >= last) return e;
-    const int k = at < per_head ? 0 : (int)((unsigned)at / (unsigned)per_head), head = head0 + k, r = at - k * per_head;
+    const int k = at < per_head ? 0 : (int)((unsigned)at / (unsigned)per_head), r = at - k * per_head;
     const int b = sequence_at(s, p.batch, r), page = r - s.prefix[b];
-    const int phys = load_dep(p.block_table + (size_t)b * p.max_pages + page);
-    int tokens = min(kPage, s.ctx[b] - page * kPage);
-    e.unit = head << kSequenceBits | b;
-    e.info = (page == 0 || at == first ? kFirst : 0) | (page + 1 == s.prefix[b + 1] - s.prefix[b] || at + 1 == last ? kLast : 0);
-    if (phys < 0 || phys >= p.num_pages) {
-        atomicOr(p.status, WC_DEV_BAD_PAGE);
-        e.row = head;
-        tokens = 0;
-    } else {
-        e.row = phys * p.num_kv_heads + head;
-        e.ks = p.scale[0] ? load_dep(p.scale[0] + e.row) : 1.0f;
-        e.vs = p.scale[1] ? load_dep(p.scale[1] + e.row) : 1.0f;
-    }
-    e.info |= tokens;
+    e.row = load_dep(p.block_table + (size_t)b * p.max_pages + page);
+    e.unit = (head0 + k) << kSequenceBits | b;
+    e.info = min(kPage, s.ctx[b] - page * kPage) | (page == 0 || at == first ? kFirst : 0) |
+             (page + 1 == s.prefix[b + 1] - s.prefix[b] || at + 1 == last ? kLast : 0);
     return e;
+}
+
+__device__ __forceinline__ void page_resolve(const BlockAttentionParams& p, PageEntry& e) {
+    const int phys = e.row;
+    const bool there = phys >= 0 && phys < p.num_pages;
+    if (!there) {
+        atomicOr(p.status, WC_DEV_BAD_PAGE);
+        e.info &= ~kTokens;
+    }
+    e.row = (there ? phys * p.num_kv_heads : 0) + (e.unit >> kSequenceBits);
+    if (p.scale[0]) {
+        e.ks = load_dep(p.scale[0] + e.row);
+        e.vs = load_dep(p.scale[1] + e.row);
+    } else {
+        e.ks = 1.0f;
+    }
 }
 
 // A head's query row as B fragments: lane (g, t) holds channels 32 t .. 32 t + 31 of query head g, in
@@ -258,8 +265,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
     if (threadIdx.x < 2) s.open[threadIdx.x] = 0;
     __syncwarp();
     uint8_t* stage0 = ring + warp * kStages * kStageBytes;
-    PageEntry cur = page_entry(p, s, head0, per_head, first + lane, first, last), next = {};
-    if (n > 32) next = page_entry(p, s, head0, per_head, first + 32 + lane, first, last);
+    PageEntry cur = page_find(p, s, head0, per_head, first + lane, first, last), next = {};
+    page_resolve(p, cur);
     int issued = 0;
     auto issue = [&](int i, int row) {   // page i of the warp's range
         issued = i + 1;
@@ -276,7 +283,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         const int row = __shfl_sync(0xffffffffu, cur.row, i);
         if (i < n) issue(i, row);
     }
-    if (warp == kWarps - 1 && lane < 2) {   // while the first pages come
+    if (n > 32) next = page_find(p, s, head0, per_head, first + 32 + lane, first, last);   // while the first pages come
+    if (warp == kWarps - 1 && lane < 2) {
         const int at = lane ? e - 1 : a, k = at < per_head ? 0 : (int)((unsigned)at / (unsigned)per_head);
         const int b = sequence_at(s, p.batch, at - k * per_head);
         Unit u = {(head0 + k) << kSequenceBits | b, k * per_head + s.prefix[b], k * per_head + s.prefix[b + 1], 0, 0};
@@ -433,9 +441,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                 if (lane == 0) s.entry[2 * warp + final] = unit;
             }
         }
+        if (from == 15 && i + 17 < n) page_resolve(p, next);
         if (from == 31) {
             cur = next;
-            if (i + 33 < n) next = page_entry(p, s, head0, per_head, first + i + 33 + lane, first, last);
+            if (i + 33 < n) next = page_find(p, s, head0, per_head, first + i + 33 + lane, first, last);
         }
     }
     if (!ok) {   // copies still in flight end before the CTA does (bounded again)
@@ -465,16 +474,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                               : *reinterpret_cast<const float2*>(cta_slots + (2 + (lane >> 1)) * slot_floats(p.group) + p.group * kHeadDim + 2 * warp);
             const float top = warp_max(ml.x), f = fast_exp2(ml.x - top), sum = warp_sum(f * ml.y);
             float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (members == (0xAAAAAAAAu >> (32 - 2 * kWarps))) {
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w)
+#pragma unroll 4
+            for (int w = 0; w < kWarps; ++w)
+                if (members >> (2 * w + 1) & 1)
                     fma4(o, __shfl_sync(0xffffffffu, f, 2 * w + 1), *reinterpret_cast<const float4*>(rows + w * kPitch + 4 * lane));
-            } else {
-                for (uint32_t rest = members; rest; rest &= rest - 1) {
-                    const int k = __ffs(rest) - 1;
-                    const float* x = k & 1 ? rows + (k >> 1) * kPitch : cta_slots + (2 + (k >> 1)) * slot_floats(p.group) + warp * kHeadDim;
-                    fma4(o, __shfl_sync(0xffffffffu, f, k), *reinterpret_cast<const float4*>(x + 4 * lane));
-                }
+            for (uint32_t rest = members & 0x55555555u; rest; rest &= rest - 1) {
+                const int k = __ffs(rest) - 1;
+                fma4(o, __shfl_sync(0xffffffffu, f, k), *reinterpret_cast<const float4*>(cta_slots + (2 + (k >> 1)) * slot_floats(p.group) + warp * kHeadDim + 4 * lane));
             }
             const bool before = unit == s.ends[0].id && s.ends[0].start < a, after = unit == s.ends[1].id && s.ends[1].end > e;
             if (!before && !after) {
