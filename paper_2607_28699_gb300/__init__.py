@@ -597,7 +597,7 @@ def block_append(desc: BlockDesc, k: torch.Tensor, v: torch.Tensor, ctx_lens: to
         if q.shape[0] != n_tok:
             raise ValueError("k and q must have the same number of tokens")
         if q_out is None:
-            q_out = q.new_empty((n_tok, desc.num_q_heads, 128))
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif q_out.shape != q.shape or q_out.dtype != q.dtype or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous and have q's shape and type")
         qp, op = q.data_ptr(), q_out.data_ptr()
@@ -621,15 +621,14 @@ def block_append(desc: BlockDesc, k: torch.Tensor, v: torch.Tensor, ctx_lens: to
 
 
 def _attention_out(desc, q, out, lse, return_lse):
-    n_tok = q.shape[0]
     if out is None:
-        out = q.new_empty((n_tok, desc.num_q_heads, 128))
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
         raise ValueError("out must be contiguous and have q's shape and type")
     if lse is None:
         if return_lse:
-            lse = torch.empty(n_tok, desc.num_q_heads, dtype=torch.float32, device=q.device)
-    elif lse.dtype != torch.float32 or lse.numel() != n_tok * desc.num_q_heads or not lse.is_contiguous():
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.numel() != q.shape[0] * desc.num_q_heads or not lse.is_contiguous():
         raise ValueError("lse must be contiguous float32 [n_tok, num_q_heads]")
     return out, lse
 
