@@ -310,3 +310,54 @@ def test_reads_the_fp8_layer_cache():
     assert (got[-1].float() - want[0]).abs().max() <= 2.0 ** -9 * float(v.abs().max())
     got = wc.block_decode_attention(bd, q[-1:], bt, lens, bc, ws)
     assert (got[0].float() - want[0]).abs().max() <= 2.0 ** -9 * float(v.abs().max())
+
+
+@pytest.mark.parametrize("hkv", [5, 160])
+def test_decode_heads_and_shares(hkv):
+    """Head counts that do not divide the SMs, or exceed them, with one sequence and with several."""
+    run(24, R.INT8, torch.float16, [260], hkv, hkv)
+    run(25, R.E4M3, torch.bfloat16, [100, 0, 37, 300], hkv, hkv)
+
+
+def test_decode_thousands_of_sequences():
+    """More sequences than one launch holds."""
+    rng = np.random.default_rng(26)
+    run(26, R.INT8, torch.float16, [int(c) for c in rng.integers(0, 40, 2600)], 2, 1)
+
+
+@pytest.mark.parametrize("hq,hkv", [(7, 1), (16, 1)])
+def test_extend_splits(hq, hkv):
+    """Few rows over a long context: the context is split over many CTAs, at lengths that do not divide evenly."""
+    run(27, R.E4M3, torch.float16, [9001], hq, hkv, new=[3])
+    run(28, R.INT8, torch.bfloat16, [4100, 130, 2000], hq, hkv, new=[2, 1, 5], causal=False)
+
+
+def test_one_workspace_for_all_calls():
+    """A workspace of the largest call serves smaller ones of other shapes, in any order."""
+    wc, desc, bt, cache, q = setup(29, R.INT8, torch.float16, [700, 900, 40, 333], 8, 2, [60, 20, 40, 3])
+    gpu = R.to_gpu(cache, R.INT8)
+    ws = wc.BlockWorkspace(desc, 4, q.shape[0], bt.shape[1])
+    args = (cache["k_codes"], cache["v_codes"], cache["k_scale"], cache["v_scale"], R.INT8, SCALE)
+    ctx = [700, 900, 40, 333]
+
+    def decode(pick):
+        qd, btd, cd = q[:len(pick)].clone(), bt[pick], [ctx[b] for b in pick]
+        out, lse = wc.block_decode_attention(desc, qd.cuda(), torch.from_numpy(btd).cuda(), torch.tensor(cd, dtype=torch.int32).cuda(), gpu, ws, return_lse=True)
+        R.check_attention(out, lse, R.attention(qd.double().numpy(), list(range(len(pick) + 1)), btd, cd, *args, False), torch.float16)
+
+    def extend(pick, new):
+        n = sum(new)
+        cu = [0] + np.cumsum(new).tolist()
+        qd, btd, cd = q[:n].clone(), bt[pick], [ctx[b] for b in pick]
+        out, lse = wc.block_extend_attention(desc, qd.cuda(), torch.tensor(cu, dtype=torch.int32).cuda(), torch.from_numpy(btd).cuda(),
+                                             torch.tensor(cd, dtype=torch.int32).cuda(), gpu, ws, return_lse=True)
+        R.check_attention(out, lse, R.attention(qd.double().numpy(), cu, btd, cd, *args, True), torch.float16)
+
+    decode([0, 1, 2, 3])
+    extend([1], [3])
+    decode([1])
+    extend([0, 1, 2, 3], [60, 20, 40, 3])
+    decode([3, 0])
+    extend([1, 0], [20, 1])
+    decode([1, 2, 3])
+    assert wc.read_status(ws) == 0
