@@ -459,25 +459,30 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
     }
     __syncthreads();
 
-    // the CTA's unfinished results (lane k looks after entry k; those of one unit follow each other), a query
-    // head per warp
+    // the CTA's unfinished results (lane k looks after entry k; those of one unit follow each other): a query head per
+    // warp, and as many units at a time as there are warps for
+    const int parts = kWarps / p.group, part = warp / p.group, hq = warp - part * p.group;   // warps per query head
     auto finish = [&](int unit, int hq, float4 o, float m, float l) {
         const int head = unit >> kSequenceBits, b = unit & ((1 << kSequenceBits) - 1);
         store_output(p, (size_t)b * p.num_q_heads + head * p.group + hq, lane, o, m, l);
     };
-    if (warp < p.group) {
+    if (part < parts) {
         const int mine = lane < 2 * kWarps ? s.entry[lane] : -1;
-        const float* rows = reinterpret_cast<const float*>(ring) + warp * kRow;   // of the warps' last results
+        const float* rows = reinterpret_cast<const float*>(ring) + hq * kRow;   // of the warps' last results
         constexpr int kPitch = kStages * kStageBytes / 4;
+        int turn = 0;
         for (uint32_t left = __ballot_sync(0xffffffffu, mine >= 0); left;) {
             const int unit = __shfl_sync(0xffffffffu, mine, __ffs(left) - 1);
             const bool member = mine == unit;
             const uint32_t members = __ballot_sync(0xffffffffu, member);
             left &= ~members;
+            const bool other = turn != part;
+            turn = turn + 1 == parts ? 0 : turn + 1;
+            if (other) continue;
             float2 ml = make_float2(kNoMax, 0.0f);
             if (member)
                 ml = lane & 1 ? *reinterpret_cast<const float2*>(rows + (lane >> 1) * kPitch + kHeadDim)
-                              : *reinterpret_cast<const float2*>(cta_slots + (2 + (lane >> 1)) * slot_floats(p.group) + p.group * kHeadDim + 2 * warp);
+                              : *reinterpret_cast<const float2*>(cta_slots + (2 + (lane >> 1)) * slot_floats(p.group) + p.group * kHeadDim + 2 * hq);
             const float top = warp_max(ml.x), f = fast_exp2(ml.x - top), sum = warp_sum(f * ml.y);
             float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
@@ -486,19 +491,19 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                     fma4(o, __shfl_sync(0xffffffffu, f, 2 * w + 1), *reinterpret_cast<const float4*>(rows + w * kPitch + 4 * lane));
             for (uint32_t rest = members & 0x55555555u; rest; rest &= rest - 1) {
                 const int k = __ffs(rest) - 1;
-                fma4(o, __shfl_sync(0xffffffffu, f, k), *reinterpret_cast<const float4*>(cta_slots + (2 + (k >> 1)) * slot_floats(p.group) + warp * kHeadDim + 4 * lane));
+                fma4(o, __shfl_sync(0xffffffffu, f, k), *reinterpret_cast<const float4*>(cta_slots + (2 + (k >> 1)) * slot_floats(p.group) + hq * kHeadDim + 4 * lane));
             }
             const bool before = unit == s.ends[0].id && s.ends[0].start < a, after = unit == s.ends[1].id && s.ends[1].end > e;
             if (!before && !after) {
-                finish(unit, warp, o, top, sum);
+                finish(unit, hq, o, top, sum);
                 continue;
             }
             const int which = before ? 0 : 1;
             float* slot = cta_slots + which * slot_floats(p.group);
-            *reinterpret_cast<float4*>(slot + warp * kHeadDim + 4 * lane) = o;
+            *reinterpret_cast<float4*>(slot + hq * kHeadDim + 4 * lane) = o;
             if (lane == 0) {
-                *reinterpret_cast<float2*>(slot + p.group * kHeadDim + 2 * warp) = make_float2(top, sum);
-                if (warp == 0) s.open[which] = 1;
+                *reinterpret_cast<float2*>(slot + p.group * kHeadDim + 2 * hq) = make_float2(top, sum);
+                if (hq == 0) s.open[which] = 1;
             }
         }
     }
@@ -511,7 +516,6 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
     }
     __syncthreads();
     float* rows = reinterpret_cast<float*>(ring);
-    const int parts = kWarps / p.group, part = warp / p.group, hq = warp - part * p.group;   // warps per query head
     for (int which = 0; which < 2; ++which) {
         if (!s.open[which]) continue;
         const int unit = s.ends[which].id, c0 = cta0 + s.ends[which].c0, c1 = cta0 + s.ends[which].c1;
