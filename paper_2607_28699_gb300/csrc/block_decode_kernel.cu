@@ -14,11 +14,12 @@
 // that reaches over several leave partial results, and the last of them to arrive merges these
 // (in the order of the pages, so the result does not depend on which one it is).
 //
-// GB300, 4 KV heads of 7 query heads: 32 sequences of 4k to 32k 113 us (5.3 TB/s, 0.78 of the measured copy rate: the
-// page loop reads 7 TB/s, the rest is the first pages' latency and the merges), 16 of 4k to 8k 35 us, one of 32k 20.5 us
+// GB300, 4 KV heads of 7 query heads: 32 sequences of 4k to 32k 107 us (5.65 TB/s, 0.83 of the measured copy rate: the
+// page loop reads 7 TB/s, the rest is the first pages' latency and the merges), 16 of 4k to 8k 33 us, one of 32k 21 us
 // (6 us page loop at the copy rate; launch and block table before it, merges in the CTA and over 38 CTAs after it).
-// 16 warps on one CTA an SM: 8 warps on two 110 / 35 / 26 us (twice the partial results), on one 131 / 37 / 23; several
-// shares per SM, taken as SMs come free, 121 / 45 / 41 (each has its own prologue and merge).
+// 16 warps on one CTA an SM (with three pages in flight each: 111 / 35 / 20.5 us; 8 warps on two CTAs 110 / 35 / 26, twice the
+// partial results; on one 131 / 37 / 23); several shares per SM, taken as SMs come free, 121 / 45 / 41 (each has its own
+// prologue and merge).
 #include "block_common.cuh"
 #include "decode_common.cuh"
 
@@ -27,7 +28,9 @@ namespace wc {
 namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32;
-constexpr int kStages = 3;
+// Pages of a warp in flight: 128 KB an SM saturate the memory; with three, what others load (block tables, partial
+// results) waits a microsecond longer behind the copies (111 / 35 us for the batches below, 107 / 33 with two).
+constexpr int kStages = 2;
 constexpr int kPageBytes = kPage * kHeadDim;           // one head's page of keys, or of values
 constexpr int kStageBytes = 2 * kPageBytes;
 constexpr int kRow = kHeadDim + 4;                     // floats of a merge row in shared memory
@@ -485,10 +488,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                               : *reinterpret_cast<const float2*>(cta_slots + (2 + (lane >> 1)) * slot_floats(p.group) + p.group * kHeadDim + 2 * hq);
             const float top = warp_max(ml.x), f = fast_exp2(ml.x - top), sum = warp_sum(f * ml.y);
             float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-            for (int w = 0; w < kWarps; ++w)
-                if (members >> (2 * w + 1) & 1)
-                    fma4(o, __shfl_sync(0xffffffffu, f, 2 * w + 1), *reinterpret_cast<const float4*>(rows + w * kPitch + 4 * lane));
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {   // no branches: sixteen loads in flight
+                float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (members >> (2 * w + 1) & 1) x = *reinterpret_cast<const float4*>(rows + w * kPitch + 4 * lane);
+                fma4(o, __shfl_sync(0xffffffffu, f, 2 * w + 1), x);
+            }
             for (uint32_t rest = members & 0x55555555u; rest; rest &= rest - 1) {
                 const int k = __ffs(rest) - 1;
                 fma4(o, __shfl_sync(0xffffffffu, f, k), *reinterpret_cast<const float4*>(cta_slots + (2 + (k >> 1)) * slot_floats(p.group) + hq * kHeadDim + 4 * lane));
