@@ -476,7 +476,7 @@ class _BlockDesc(ctypes.Structure):
                 ("rope_layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32)]
 
 
-@dataclass
+@dataclass(frozen=True)
 class BlockDesc:
     """Mirror of ``wc_block_desc``."""
     num_q_heads: int
@@ -492,9 +492,12 @@ class BlockDesc:
     def group(self):
         return self.num_q_heads // self.num_kv_heads
 
+    def __post_init__(self):
+        object.__setattr__(self, "_c", _BlockDesc(self.head_dim, self.num_q_heads, self.num_kv_heads, self.page_size,
+                                                  self.num_pages, self.code, self.rope_layout, self.rotary_dim))
+
     def c(self):
-        return _BlockDesc(self.head_dim, self.num_q_heads, self.num_kv_heads, self.page_size, self.num_pages,
-                          self.code, self.rope_layout, self.rotary_dim)
+        return self._c
 
 
 @dataclass(frozen=True)
@@ -534,8 +537,7 @@ class BlockWorkspace:
     """Zero-filled device workspace for the block attention calls of up to ``n_tok`` query tokens."""
 
     def __init__(self, desc: BlockDesc, batch: int, n_tok: int, max_pages: int, device="cuda"):
-        d = desc.c()
-        self.nbytes = lib.wc_block_workspace_size(ctypes.byref(d), batch, n_tok, max_pages)
+        self.nbytes = lib.wc_block_workspace_size(ctypes.byref(desc._c), batch, n_tok, max_pages)
         if self.nbytes == 0:
             raise WitCertError(1, lib.wc_last_error().decode())
         self.buf = torch.zeros(self.nbytes + 256, dtype=torch.uint8, device=device)
@@ -608,9 +610,8 @@ def block_append(desc: BlockDesc, k: torch.Tensor, v: torch.Tensor, ctx_lens: to
                 or sin.dtype != torch.float32 or not cos.is_contiguous() or not sin.is_contiguous()):
             raise ValueError(f"cos and sin must be contiguous float32 [positions, {desc.rotary_dim // 2}]")
         num_positions, cp, sp = shape[0], cos.data_ptr(), sin.data_ptr()
-    d = desc.c()
     st = lib.wc_block_append(
-        ctypes.byref(d), act, k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, n_tok,
+        ctypes.byref(desc._c), act, k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, n_tok,
         None if cu_new is None else _ints(cu_new, batch + 1, "cu_new"), _ints(block_table, batch * max_pages, "block_table"),
         max_pages, _ints(ctx_lens, batch, "ctx_lens"), batch,
         None if positions is None else _ints(positions, n_tok, "positions"), cp, sp, num_positions,
@@ -627,7 +628,7 @@ def _attention_out(desc, q, out, lse, return_lse):
         raise ValueError("out must be contiguous and have q's shape and type")
     if lse is None:
         if return_lse:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+            lse = torch.empty(q.shape[0], desc.num_q_heads, dtype=torch.float32, device=q.device)
     elif lse.dtype != torch.float32 or lse.numel() != q.shape[0] * desc.num_q_heads or not lse.is_contiguous():
         raise ValueError("lse must be contiguous float32 [n_tok, num_q_heads]")
     return out, lse
@@ -647,9 +648,8 @@ def block_decode_attention(desc: BlockDesc, q: torch.Tensor, block_table: torch.
     if q.shape[0] != batch:
         raise ValueError(f"q must have one token per sequence ({batch}), got {q.shape[0]}")
     out, lse = _attention_out(desc, q, out, lse, return_lse)
-    d = desc.c()
     st = lib.wc_block_decode_attention(
-        ctypes.byref(d), act, q.data_ptr(), qs, _ints(block_table, batch * max_pages, "block_table"), max_pages,
+        ctypes.byref(desc._c), act, q.data_ptr(), qs, _ints(block_table, batch * max_pages, "block_table"), max_pages,
         _ints(ctx_lens, batch, "ctx_lens"), batch, *_block_cache(desc, cache),
         _SCALE_128 if softmax_scale is None else softmax_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
         ws.view.data_ptr(), ws.nbytes, _stream(stream))
@@ -668,9 +668,8 @@ def block_extend_attention(desc: BlockDesc, q: torch.Tensor, cu_q: torch.Tensor,
     act = _ACT.get(q.dtype)
     qs = _rows(q, desc.num_q_heads, act, "q")
     out, lse = _attention_out(desc, q, out, lse, return_lse)
-    d = desc.c()
     st = lib.wc_block_extend_attention(
-        ctypes.byref(d), act, q.data_ptr(), qs, q.shape[0], _ints(cu_q, batch + 1, "cu_q"),
+        ctypes.byref(desc._c), act, q.data_ptr(), qs, q.shape[0], _ints(cu_q, batch + 1, "cu_q"),
         _ints(block_table, batch * max_pages, "block_table"), max_pages, _ints(ctx_lens, batch, "ctx_lens"), batch,
         *_block_cache(desc, cache), _SCALE_128 if softmax_scale is None else softmax_scale, int(causal),
         out.data_ptr(), None if lse is None else lse.data_ptr(), ws.view.data_ptr(), ws.nbytes, _stream(stream))
