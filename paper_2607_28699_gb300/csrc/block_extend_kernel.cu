@@ -667,10 +667,10 @@ __global__ void __launch_bounds__(256) block_extend_merge_kernel(const __grid_co
 constexpr int kMaxSplits = 64, kMaxCtas = 4;   // of a row; of a call that splits rows, per SM
 
 struct ExtendPlan {
-    long long blocks;   // tile pairs, an upper bound
+    long long blocks;   // tile pairs, an upper bound: find_work's numbering leaves some to nobody
     int splits;
-    ExtendPlan(int batch, int n_tok, int num_kv_heads, int group, int max_pages, int num_sms) {
-        blocks = std::min<long long>((long long)n_tok * group / (kTiles * kTile) + batch, n_tok);
+    ExtendPlan(bool ragged, int batch, int n_tok, int num_kv_heads, int group, int max_pages, int num_sms) {
+        blocks = ragged ? (long long)n_tok * group / (kTiles * kTile) + batch : batch;
         // the split count that takes the fewest tile steps: waves x (tiles of a split + a fixed part of about two)
         const long long ctas = blocks * num_kv_heads;
         const int tiles = (max_pages + kPages - 1) / kPages;
@@ -697,7 +697,7 @@ cudaError_t launch_block_extend(const BlockAttentionParams& p, int code, int num
     static PerDevice<Configured, cudaError_t> configured[2];
     auto* kernel = code == WC_CODE_INT8 ? block_extend_kernel<WC_CODE_INT8> : block_extend_kernel<WC_CODE_E4M3>;
     if (cudaError_t e = configure(configured[code == WC_CODE_INT8], kernel, kSmem)) return e;
-    const ExtendPlan plan(p.batch, p.n_tok, p.num_kv_heads, p.group, p.max_pages, num_sms);
+    const ExtendPlan plan(p.cu_q != nullptr, p.batch, p.n_tok, p.num_kv_heads, p.group, p.max_pages, num_sms);
     const long long cells = (long long)p.n_tok * p.num_q_heads;
     ExtendArgs args;
     args.p = p;

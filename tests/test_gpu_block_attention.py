@@ -361,3 +361,12 @@ def test_one_workspace_for_all_calls():
     extend([1, 0], [20, 1])
     decode([1, 2, 3])
     assert wc.read_status(ws) == 0
+
+
+@pytest.mark.parametrize("group", [1, 7])
+def test_extend_mostly_empty_batches(group):
+    """Far fewer query tokens than sequences, the ones with tokens among the last."""
+    ctx = [20] * 300
+    new = [0] * 300
+    ctx[150], new[150], ctx[298], new[298], ctx[299], new[299] = 400, 2, 33, 1, 700, 30
+    run(30, R.INT8, torch.float16, ctx, group, 1, new=new)
