@@ -98,6 +98,10 @@ __device__ __forceinline__ uint16_t float_to_act(float x, bool bf16) {
     return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
 }
 
+// A page's value scale below this (0, as a rule) counts as 0: its codes are taken as 0 and the scale as 1, since the
+// kernels work with its logarithm and its reciprocal.
+constexpr float kLeastValueScale = 0x1p-126f;
+
 // log(sum of 2^m l), -inf for an empty sum.
 __device__ __forceinline__ float log_sum(float m, float l) {
     return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;

@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         const int info = __shfl_sync(0xffffffffu, cur.info, from);
         const float ks = __shfl_sync(0xffffffffu, cur.ks, from) * p.scale_log2;
         float vs = __shfl_sync(0xffffffffu, cur.vs, from);
-        const bool no_values = vs == 0.0f;   // the codes count as 0 then, whatever they are
+        const bool no_values = vs < kLeastValueScale;
         if (no_values) vs = 1.0f;
         if (info & kFirst) {
             const int unit = __shfl_sync(0xffffffffu, cur.unit, from);

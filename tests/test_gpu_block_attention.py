@@ -370,3 +370,11 @@ def test_extend_mostly_empty_batches(group):
     new = [0] * 300
     ctx[150], new[150], ctx[298], new[298], ctx[299], new[299] = 400, 2, 33, 1, 700, 30
     run(30, R.INT8, torch.float16, ctx, group, 1, new=new)
+
+
+@pytest.mark.parametrize("new", [None, [33]])
+def test_subnormal_value_scales(new):
+    """Value scales below the least normal number: the page's values count as 0 (they are, next to the others), its keys do not."""
+    def edit(cache, bt, q):
+        cache["v_scale"][bt[0, ::2]] = 1e-40
+    run(31, R.INT8, torch.float16, [300], 4, 1, new=new, edit=edit)
