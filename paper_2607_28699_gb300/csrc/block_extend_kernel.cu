@@ -15,8 +15,8 @@
 // A softmax thread moves its running maximum (and its row of O) only when a logit passes it by 2^8.
 //
 // GB300, 28 query / 4 KV heads: 4096 tokens at the end of 32k, int8 codes, fp16: 1209 us, 1491 TFLOP/s (0.78 of the
-// measured cuBLAS bf16 rate); an 8k prompt from e4m3, bf16: 358 us, 1345 TFLOP/s (half of what is left is the 6 us that a
-// CTA needs before its first and after its last product); 16 sequences of 5 drafted tokens at 4k to 8k 65 us, where
+// measured cuBLAS bf16 rate); an 8k prompt from e4m3, bf16: 358 us, 1345 TFLOP/s (11 us of a CTA's 65 pass
+// before its first and after its last product); 16 sequences of 5 drafted tokens at 4k to 8k 65 us, where
 // one tile of rows leaves its softmax (1450 cycles a step) and its products (1100) to follow each other.  A step of two
 // tiles costs 3050 cycles against the MMAs' 2050: what the issuing warp waits for is not hidden, as few MMAs queue.
 // Tried and slower: a warp per tile issuing MMAs (1480 us, taking turns by a barrier 1391), the copies'
