@@ -35,7 +35,7 @@ constexpr int kSoftmaxWarps = 4 * kTiles, kConvertWarps = 4;
 constexpr int kMmaWarp = kSoftmaxWarps + kConvertWarps, kLoadWarp = kMmaWarp + 1;
 constexpr int kThreads = 32 * (kMmaWarp + 4);
 // Registers: 128 a thread at launch, 512 threads; a softmax thread holds 64 packed weights and 32 logits and
-// takes what the MMA warps give: 256 x 176 + 128 x 80 + 128 x 80 = 512 x 128.
+// takes what the others give: 256 x 176 + 128 x 80 + 128 x 80 = 512 x 128.
 constexpr int kSoftmaxRegs = 176, kConvertRegs = 80, kMmaRegs = 80;
 static_assert(kSoftmaxWarps * 32 * kSoftmaxRegs + kConvertWarps * 32 * kConvertRegs + 4 * 32 * kMmaRegs <= kThreads * 128);
 constexpr int kOperand = kTile * kHeadDim * 2;   // bytes of a [128][128] fp16 operand: two blocks of 64 channels
