@@ -242,6 +242,16 @@ __device__ __forceinline__ void rotate_queries(const BlockAppendParams& p, int r
     const Chunks<kHalfLayout> at(i, rot >> 4);
     const char* src = static_cast<const char*>(p.q) + 2 * (size_t)row * p.q_stride;
     char* dst = static_cast<char*>(p.q_out) + 2 * (size_t)row * p.num_q_heads * kHeadDim;
+    constexpr int kAhead = 4;   // steps of four heads in flight
+    Raw raw[kAhead];
+    auto fetch = [&](int h0) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            raw[j] = {};
+            if (h0 + 4 * j < end) raw[j] = load_raw(src + 2 * (size_t)(h0 + 4 * j) * kHeadDim, at.a, at.b);
+        }
+    };
+    fetch(head0 + sub);   // the rows do not wait for whose they are
     int b = row;
     if (p.cu_new) b = warp_find_last(p.batch, row, [&](int s) { return (long long)load_dep(p.cu_new + s); });
     Sequence s;
@@ -252,18 +262,13 @@ __device__ __forceinline__ void rotate_queries(const BlockAppendParams& p, int r
     if (bad && lane == 0) report(p, WC_DEV_BAD_POSITION);
     Trig trig;
     if (at.rotated && !bad) load_trig(p, position, i, trig);
-    constexpr int kAhead = 4;   // steps of four heads in flight
     for (int h0 = head0 + sub; h0 - sub < end; h0 += 4 * kAhead) {
-        Raw raw[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            raw[j] = {};
-            if (h0 + 4 * j < end && !bad) raw[j] = load_raw(src + 2 * (size_t)(h0 + 4 * j) * kHeadDim, at.a, at.b);
-        }
+        if (h0 != head0 + sub) fetch(h0);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (h0 + 4 * j >= end) continue;
             float y[16];
+            if (bad) raw[j] = {};
             rotate<kBf16, kHalfLayout>(raw[j], at.rotated && !bad, trig, y);
             uint4* out = reinterpret_cast<uint4*>(dst + 2 * (size_t)(h0 + 4 * j) * kHeadDim);
             uint32_t w[8];
