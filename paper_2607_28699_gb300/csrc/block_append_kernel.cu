@@ -6,7 +6,7 @@
 // take a third of the SM's warps (32k prompt 133 us).
 //
 // GB300, 28 query / 4 KV heads: a prompt of 32768 tokens 107 us, 5.5 TB/s of the 587 MB that it has to move (0.81 of the
-// measured copy rate; the loads' latency at 24 warps an SM), 16 ragged chunks of up to 1023 tokens (40 / 8 heads) 49 us;
+// measured copy rate; the loads' latency at 24 warps an SM), 16 ragged chunks of up to 1023 tokens (40 / 8 heads) 48 us;
 // one token 6 us, all of it launch and a chain of five loads (context, block table, scale, angles, row).
 #include "block_common.cuh"
 
