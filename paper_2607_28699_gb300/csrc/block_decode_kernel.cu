@@ -99,8 +99,9 @@ __device__ __forceinline__ int context(const BlockAttentionParams& p, int b, boo
     return ctx;
 }
 
-// Contexts and exclusive prefix sums of their pages.  Up to 32 sequences each warp finds them by itself
-// (all write the same values), more are shared out over the CTA.
+// Contexts and exclusive prefix sums of their pages.  Up to 32 sequences each warp finds them by itself and goes on
+// without a barrier: a place is written once by each, with the sum that every warp writes there, since others may be
+// reading it.  More are shared out over the CTA.
 __device__ __forceinline__ void page_prefix(const BlockAttentionParams& p, Shared& s, bool tell) {
     const int tid = threadIdx.x, lane = tid & 31;
     const bool by_warp = p.batch <= 32;
@@ -110,7 +111,7 @@ __device__ __forceinline__ void page_prefix(const BlockAttentionParams& p, Share
     for (int b = b0; b < b1; ++b) {
         const int ctx = context(p, b, tell);
         s.ctx[b] = ctx;
-        s.prefix[b] = mine;
+        if (!by_warp) s.prefix[b] = mine;
         mine += (ctx + kPage - 1) >> 4;
     }
     int incl = mine;
