@@ -29,16 +29,16 @@ __device__ __forceinline__ bool sequence(const BlockAppendParams& p, int b, Sequ
     s.lo = p.cu_new ? load_dep(p.cu_new + b) : b;
     const int hi = p.cu_new ? load_dep(p.cu_new + b + 1) : b + 1;
     const int ctx = load_dep(p.ctx_lens + b);
-    s.n = hi - s.lo;
-    s.start = ctx - s.n;
     if (s.lo < 0 || hi < s.lo || hi > p.n_tok) {
         if (kTell) report(p, WC_DEV_BAD_ROWS);
         return false;
     }
-    if (s.n > 0 && (s.start < 0 || ctx > (long long)p.max_pages * kPage)) {
+    s.n = hi - s.lo;
+    if (s.n > 0 && (ctx < s.n || ctx > (long long)p.max_pages * kPage)) {   // compared, not subtracted: any int32 may come
         if (kTell) report(p, WC_DEV_BAD_CTX);
         return false;
     }
+    s.start = ctx - s.n;
     return s.n > 0;
 }
 
