@@ -532,7 +532,8 @@ typedef struct {
  *   q, q_out     [n_tok][Hq][128]; q with q_stride, q_out dense; both NULL: no queries
  *   cu_new       [batch + 1] int32, ascending, cu_new[batch] <= n_tok; NULL: one token per
  *                sequence (n_tok = batch)
- *   block_table  [batch][max_pages] int32; entries past a sequence's pages are not read
+ *   block_table  [batch][max_pages] int32, max_pages at most 2^27 - 64 (the attention calls' too);
+ *                entries past a sequence's pages are not read
  *   ctx_lens     [batch] int32, with the new tokens
  *   positions    [n_tok] int32 rotary positions; NULL: the logical positions
  *   cos_table, sin_table  [num_positions][rotary_dim / 2] fp32; NULL if rotary_dim is 0

@@ -11,6 +11,8 @@ using wc::fail;
 namespace {
 
 constexpr int kMaxBlockGroup = 128;
+// The kernels' int32 positions reach up to a tile of keys past a context's end.
+constexpr int kMaxTablePages = (1 << 27) - 64;
 constexpr double kLog2e = 1.4426950408889634;
 
 wc_status check_block_desc(const wc_block_desc* d) {
@@ -49,7 +51,8 @@ wc_status check_sizes(int32_t act_type, int32_t batch, int32_t n_tok, int32_t ma
     if (batch < 0 || batch > 65535) return fail(WC_ERR_INVALID_ARG, "batch must be in [0, 65535] (got %d)", batch);
     if (n_tok < 0) return fail(WC_ERR_INVALID_ARG, "n_tok must be >= 0 (got %d)", n_tok);
     if (max_pages < 1) return fail(WC_ERR_INVALID_ARG, "max_pages must be positive (got %d)", max_pages);
-    if ((long long)max_pages * wc::kPage > 0x7FFFFFFFLL) return fail(WC_ERR_UNSUPPORTED, "max_pages too large");
+    if (max_pages > kMaxTablePages)
+        return fail(WC_ERR_UNSUPPORTED, "max_pages must be at most %d (got %d)", kMaxTablePages, max_pages);
     return WC_OK;
 }
 
