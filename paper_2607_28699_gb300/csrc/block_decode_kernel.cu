@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         const float ks = __shfl_sync(0xffffffffu, cur.ks, from) * p.scale_log2;
         float vs = __shfl_sync(0xffffffffu, cur.vs, from);
         const bool no_values = vs < kLeastValueScale;
-        if (no_values) vs = 1.0f;
+        if (no_values) vs = kNoValueScale;
         if (info & kFirst) {
             const int unit = __shfl_sync(0xffffffffu, cur.unit, from);
             const float f = load_queries(p, unit & ((1 << kSequenceBits) - 1), unit >> kSequenceBits, q);

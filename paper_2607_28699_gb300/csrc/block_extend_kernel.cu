@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                         Meta& meta = s.meta[j % kMetaStages];
                         const bool outside = !there && page0 + j * kPages < pages;
                         const int tokens = there ? min(kPage, w.ctx - (page0 + j * kPages) * kPage) : 0;
-                        const float of = vs < kLeastValueScale ? 1.0f : vs;
+                        const float of = vs < kLeastValueScale ? kNoValueScale : vs;
                         meta.ks[lane] = ks * p.scale_log2;
                         meta.bias[lane] = outside ? -INFINITY : log2f(of);
                         meta.inv[lane] = __frcp_rn(of);
