@@ -176,7 +176,7 @@ __device__ __forceinline__ void page_resolve(const BlockAttentionParams& p, Page
         e.info &= ~kTokens;
     }
     e.row = (there ? phys * p.num_kv_heads : 0) + (e.unit >> kSequenceBits);
-    if (p.scale[0]) {
+    if (there && p.scale[0]) {
         e.ks = load_dep(p.scale[0] + e.row);
         e.vs = load_dep(p.scale[1] + e.row);
     } else {
