@@ -524,7 +524,7 @@ typedef struct {
  * What a page holds past the new tokens is left as it is and not looked at, so
  * a token appended again at an earlier position (a draft that was rejected)
  * replaces the one that was there.  A row with infinities or NaN makes its page's scale that (sticky until
- * the page is begun anew) and its codes 0, and attention over the page NaN.
+ * the page is begun anew) and its codes 0, and attention NaN for the query rows that see any of the page (lse: of K only).
  * A page written by the call belongs to one sequence (as with wc_metered_decode_attention_append).
  *
  *   k, v         [n_tok][Hkv][128] act_type, device; k_stride, v_stride elements from one

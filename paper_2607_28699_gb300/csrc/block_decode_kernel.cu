@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         const int info = __shfl_sync(0xffffffffu, cur.info, from);
         const float ks = __shfl_sync(0xffffffffu, cur.ks, from) * p.scale_log2;
         float vs = __shfl_sync(0xffffffffu, cur.vs, from);
-        const bool no_values = vs < kLeastValueScale;
+        const bool lost = !(vs < INFINITY), no_values = lost || vs < kLeastValueScale;   // lost: infinity or NaN
         if (no_values) vs = kNoValueScale;
         if (info & kFirst) {
             const int unit = __shfl_sync(0xffffffffu, cur.unit, from);
@@ -401,6 +401,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                 codes4_to_h2<kCode>(d[2 * h + 1], af[1], af[3]);
                 mma16816(acc[2 * j + h], af, b0, b1);
             }
+        }
+        if (lost) {   // the output is; the sum of weights does not depend on values
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[j][c] = NAN;
         }
         __syncwarp();
         // the stage is free: the page kStages on

@@ -59,6 +59,7 @@ struct Shared {
     uint64_t ready[kTiles][2];
     Meta meta[kMetaStages];
     uint32_t tmem;
+    int nan_from;   // position of the first page whose values are NaN
     int abandoned;
 };
 constexpr int kSmem = (kTiles + 4) * kOperand + 2 * kCodes + (int)sizeof(Shared) + 1024;
@@ -293,6 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
             for (int k = 0; k < 2; ++k) mbar_init(&s.ready[i][k], 128 + 2 * kConvertWarps);
             mbar_init(&s.o_full[i], 1);
         }
+        s.nan_from = INT_MAX;
         s.abandoned = 0;
         fence_barrier_init();
     }
@@ -600,12 +602,14 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                         Meta& meta = s.meta[j % kMetaStages];
                         const bool outside = !there && page0 + j * kPages < pages;
                         const int tokens = there ? min(kPage, w.ctx - (page0 + j * kPages) * kPage) : 0;
-                        const float of = vs < kLeastValueScale ? kNoValueScale : vs;
+                        const bool lost = !(vs < INFINITY), no_values = lost || vs < kLeastValueScale;   // lost: infinity or NaN
+                        const float of = no_values ? kNoValueScale : vs;
                         meta.ks[lane] = ks * p.scale_log2;
                         meta.bias[lane] = outside ? -INFINITY : log2f(of);
                         meta.inv[lane] = __frcp_rn(of);
                         meta.tokens[0][lane] = tokens;
-                        meta.tokens[1][lane] = vs < kLeastValueScale ? 0 : tokens;
+                        meta.tokens[1][lane] = no_values ? 0 : tokens;
+                        if (lost) atomicMin(&s.nan_from, (page0 + j * kPages) * kPage);
                         if (outside) atomicOr(p.status, WC_DEV_BAD_PAGE);
                     }
                     __syncwarp();
@@ -630,6 +634,17 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     if (warp == kMmaWarp && n > 0) {
         fence_after();
         tmem_free(tmem);
+    }
+    // Rows that see values that are NaN, rarely: the products took them as 0, for the rows that do not see them.  Written here,
+    // where no role's registers have to hold what it needs.
+    if (s.nan_from < INT_MAX) {
+        for (int i = threadIdx.x; i < w.rows * kHeadDim; i += kThreads) {
+            const int row = i / kHeadDim, r = w.row0 + row;
+            if (keys_seen(p, w, r) <= s.nan_from) continue;
+            const size_t at = ((size_t)(w.lo + r / p.group) * p.num_q_heads + head * p.group + r % p.group) * kHeadDim + i % kHeadDim;
+            if (args.splits > 1) args.part_o[(size_t)blockIdx.z * p.n_tok * p.num_q_heads * kHeadDim + at] = NAN;
+            else static_cast<uint16_t*>(p.out)[at] = 0x7FFF;   // in both types
+        }
     }
 }
 
