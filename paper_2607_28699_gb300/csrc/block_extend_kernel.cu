@@ -59,8 +59,8 @@ struct Shared {
     uint64_t ready[kTiles][2];
     Meta meta[kMetaStages];
     uint32_t tmem;
-    int nan_from;   // position of the first page whose values are NaN
     int abandoned;
+    int any_nan, nan_page, nan_code[kHeadDim];   // positions of the first page, and of the first key in a channel, whose values are NaN
 };
 constexpr int kSmem = (kTiles + 4) * kOperand + 2 * kCodes + (int)sizeof(Shared) + 1024;
 static_assert(kSmem <= 227 * 1024);
@@ -294,10 +294,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
             for (int k = 0; k < 2; ++k) mbar_init(&s.ready[i][k], 128 + 2 * kConvertWarps);
             mbar_init(&s.o_full[i], 1);
         }
-        s.nan_from = INT_MAX;
-        s.abandoned = 0;
+        s.nan_page = INT_MAX;
+        s.any_nan = s.abandoned = 0;
         fence_barrier_init();
     }
+    if (threadIdx.x < kHeadDim) s.nan_code[threadIdx.x] = INT_MAX;
     grid_dep_wait();
     grid_dep_launch();
     if (p.cu_q && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0)   // one CTA reports the ranges that cannot be
@@ -477,16 +478,37 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         const int src0 = row * kHeadDim + 16 * (chunk ^ row), src1 = row * kHeadDim + 16 * ((chunk + 4) ^ row);
         const int dst0 = (32 * cw + row) * 128 + 16 * ((2 * chunk) ^ row), dst1 = (32 * cw + row) * 128 + 16 * ((2 * chunk + 1) ^ row);
         // 16 codes a lane and step (8 rows of 4 chunks, conflict-free in both layouts)
-        auto expand = [&](int side, uint8_t* op, const int* tokens) {
+        const int all_see = keys_seen(p, w, w.row0);   // keys that every row sees
+        // key0: position of the warp's first key
+        auto expand = [&](int side, uint8_t* op, const int* tokens, int key0) {
             const int have0 = tokens[2 * cw], have1 = tokens[2 * cw + 1];
-            const uint8_t* src = staged + side * kCodes + cw * (2 * kPage * kHeadDim);
+            uint8_t* src = staged + side * kCodes + cw * (2 * kPage * kHeadDim);
             uint4 x[8];   // read first: the compiler cannot tell the stores from the loads
+            for (;;) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const uint4*>(src + (i >> 1) * 1024 + (i & 1 ? src1 : src0));
-            if (min(have0, have1) < kPage) {
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const uint4*>(src + (i >> 1) * 1024 + (i & 1 ? src1 : src0));
+                if (min(have0, have1) < kPage) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (8 * ((i >> 1) & 1) + row >= (i < 4 ? have0 : have1)) x[i] = make_uint4(0, 0, 0, 0);
+                }
+                if (kCode != WC_CODE_E4M3 || side == 0 || key0 + 2 * kPage <= all_see) break;
+                // a NaN among the values would reach the rows that do not see it, times 0
+                uint32_t nan = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (8 * ((i >> 1) & 1) + row >= (i < 4 ? have0 : have1)) x[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) nan |= (word_of(x[i], k) & 0x7F7F7F7Fu) + 0x01010101u;
+                if (!__any_sync(0xffffffffu, nan & 0x80808080u)) break;
+                s.any_nan = 1;   // rarely: it counts as 0 here, and is noted for the rows that see it
+#pragma unroll 1
+                for (int i = 0; i < 8 * 16; ++i) {
+                    const int r = 8 * ((i >> 5) & 3) + row, c = chunk + 4 * ((i >> 4) & 1);   // row of the two pages, chunk of the row
+                    uint8_t* code = src + r * kHeadDim + 16 * (c ^ row) + (i & 15);
+                    if ((*code & 0x7F) != 0x7F) continue;
+                    *code = 0;
+                    if ((r & 15) < (r < kPage ? have0 : have1)) atomicMin(&s.nan_code[16 * c + (i & 15)], key0 + r);
+                }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -507,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 if (j >= 2) ok = wait(s, side ? &s.v_empty[st] : &s.k_empty[st], ((j >> 1) - 1) & 1);
                 ok = ok && wait(s, &s.codes_full[side], j & 1);
                 if (!ok) break;
-                expand(side, (side ? v_op : k_op) + st * kOperand, meta.tokens[side]);
+                expand(side, (side ? v_op : k_op) + st * kOperand, meta.tokens[side], (t0 + j) * kTile + 32 * cw);
                 fence_async();
                 __syncwarp();
                 if (lane == 0) {
@@ -609,7 +631,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                         meta.inv[lane] = __frcp_rn(of);
                         meta.tokens[0][lane] = tokens;
                         meta.tokens[1][lane] = no_values ? 0 : tokens;
-                        if (lost) atomicMin(&s.nan_from, (page0 + j * kPages) * kPage);
+                        if (lost) {
+                            atomicMin(&s.nan_page, (page0 + j * kPages) * kPage);
+                            s.any_nan = 1;
+                        }
                         if (outside) atomicOr(p.status, WC_DEV_BAD_PAGE);
                     }
                     __syncwarp();
@@ -637,10 +662,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
     }
     // Rows that see values that are NaN, rarely: the products took them as 0, for the rows that do not see them.  Written here,
     // where no role's registers have to hold what it needs.
-    if (s.nan_from < INT_MAX) {
+    if (s.any_nan) {
         for (int i = threadIdx.x; i < w.rows * kHeadDim; i += kThreads) {
             const int row = i / kHeadDim, r = w.row0 + row;
-            if (keys_seen(p, w, r) <= s.nan_from) continue;
+            if (keys_seen(p, w, r) <= min(s.nan_page, s.nan_code[i % kHeadDim])) continue;
             const size_t at = ((size_t)(w.lo + r / p.group) * p.num_q_heads + head * p.group + r % p.group) * kHeadDim + i % kHeadDim;
             if (args.splits > 1) args.part_o[(size_t)blockIdx.z * p.n_tok * p.num_q_heads * kHeadDim + at] = NAN;
             else static_cast<uint16_t*>(p.out)[at] = 0x7FFF;   // in both types
