@@ -479,7 +479,7 @@ wc_status wc_gate_joint(const float* meter_raw, const float* value_term, const f
  * cache of a serving stack, beside the metered one).  One fp32 scale for the 16
  * tokens of a page and KV head; x^ = scale * code:
  *   k_codes, v_codes [num_pages][Hkv][16][128]  int8, or fp8 e4m3fn bytes
- *   k_scale, v_scale [num_pages][Hkv]           fp32, >= 0 (v_scale below 2^-126 counts as 0)
+ *   k_scale, v_scale [num_pages][Hkv]           fp32, >= 0 (v_scale below 2^-100 counts as 0)
  * The code arrays have the layout of WC_SCHEME_FP8_E4M3's, so the attention
  * calls below also read that scheme's cache (k_scale = v_scale = NULL: scale 1).
  */

@@ -98,12 +98,13 @@ __device__ __forceinline__ uint16_t float_to_act(float x, bool bf16) {
     return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
 }
 
-// A page's value scale below this (0, as a rule) counts as 0: its codes are taken as 0.  The kernels work with a scale's
+// A page's value scale below this (0, as a rule; the append makes none) counts as 0: its codes are taken as 0.  Smaller
+// ones' reciprocals could take the sum of weights past fp32's range.  The kernels work with a scale's
 // logarithm and reciprocal, so a small one stands in for it: its page's weights enter the running maximum of weighted values
 // multiplied by it, and the sum of weights divided by it again.  A page of scale s keeps the maximum unless the other's
 // logits (log2) are 80 + log2(s) above its own (with 1 for a stand-in, a sink of zero values took usual weights out of
 // fp16's range), and the sum of weights holds what is above 2^(log2(s) - 46) of its own.
-constexpr float kLeastValueScale = 0x1p-126f, kNoValueScale = 0x1p-80f;
+constexpr float kLeastValueScale = 0x1p-100f, kNoValueScale = 0x1p-80f;
 
 // log(sum of 2^m l), -inf for an empty sum.
 __device__ __forceinline__ float log_sum(float m, float l) {
