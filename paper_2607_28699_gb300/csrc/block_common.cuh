@@ -103,17 +103,27 @@ __device__ __forceinline__ uint16_t float_to_act(float x, bool bf16) {
 // logarithm and reciprocal, so a small one stands in for it: its page's weights enter the running maximum of weighted values
 // multiplied by it, and the sum of weights divided by it again.  A page of scale s keeps the maximum unless the other's
 // logits (log2) are 80 + log2(s) above its own (with 1 for a stand-in, a sink of zero values took usual weights out of
-// fp16's range), and the sum of weights holds what is above 2^(log2(s) - 46) of its own.
+// fp16's range), and the sum of weights holds what is above 2^(log2(s) - 53) of its own.
 constexpr float kLeastValueScale = 0x1p-100f, kNoValueScale = 0x1p-80f;
+
+// Weights 2^(y - m) are rounded to fp16 for the second product.  The frame m is put kHeadroom below the largest y, and moves
+// when one passes it by kTopWeight: the largest weight lies in [2^7, 2^15], and others keep all their bits down to 2^-21
+// of it, some to 2^-32 (from 1 on: 2^-14 and 2^-25, and what a sharp head gives to many tokens in all was lost below).
+constexpr float kHeadroom = 7.0f, kTopWeight = 15.0f;
+// The sum of weights l is kept times 2^-10: with value scales from 2^-100 on and 2^20 tokens it stays within fp32's range, and
+// so do the reciprocals of the largest scales.
+constexpr float kSumUnit = 0x1p-10f;
 
 // log(sum of 2^m l), -inf for an empty sum.
 __device__ __forceinline__ float log_sum(float m, float l) {
-    return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    return l == 0.0f ? -INFINITY : (m + 10.0f + log2f(l)) * 0.6931471805599453f;
 }
+// What sums of weighted values are multiplied with.
+__device__ __forceinline__ float output_factor(float l) { return l == 0.0f ? 0.0f : __frcp_rn(l) * kSumUnit; }
 
 // A warp's output row: four channels a lane, divided by the sum of weights.
 __device__ __forceinline__ void store_output(const BlockAttentionParams& p, size_t cell, int lane, float4 o, float m, float l) {
-    const float f = l == 0.0f ? 0.0f : __frcp_rn(l);
+    const float f = output_factor(l);
     const uint32_t lo = p.bf16 ? float2_to_act2<true>(o.x * f, o.y * f) : pack_h2(o.x * f, o.y * f);
     const uint32_t hi = p.bf16 ? float2_to_act2<true>(o.z * f, o.w * f) : pack_h2(o.z * f, o.w * f);
     reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + cell * kHeadDim)[lane] = make_uint2(lo, hi);

@@ -9,7 +9,7 @@
 //     is an offset in the exponent, so 2^(y - m) is p vs at no cost, and O sums it times V's
 //     codes; the sum of weights takes p = 2^(y - m) / vs;
 //   O^T (128 x 8) += V^T P^T, 8 mma, V transposed by ldmatrix on bytes.
-// The running maximum m moves only when a logit passes it by 2^8 (one vote a page).
+// The frame m follows the running maximum lazily: it moves only when a weight would pass 2^15 (one vote a page).
 // A unit inside one warp's range is finished there, one inside a CTA's by the CTA; the CTAs of a unit
 // that reaches over several leave partial results, and the last of them to arrive merges these
 // (in the order of the pages, so the result does not depend on which one it is).
@@ -35,8 +35,7 @@ constexpr int kPageBytes = kPage * kHeadDim;           // one head's page of key
 constexpr int kStageBytes = 2 * kPageBytes;
 constexpr int kRow = kHeadDim + 4;                     // floats of a merge row in shared memory
 constexpr int kMinPages = 1;                           // per warp, before a launch takes more CTAs
-constexpr float kNoMax = -1e30f;                       // the running maximum before the first logit
-constexpr float kSlack = 8.0f;                         // log2 units a logit may pass it by
+constexpr float kNoMax = -1e30f;                       // the frame before the first logit
 
 struct DecodeArgs {
     BlockAttentionParams p;
@@ -360,13 +359,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
             if (trow + 2 >= tokens) y[2] = y[3] = -INFINITY;
         }
         const float top0 = fmaxf(y[0], y[2]), top1 = fmaxf(y[1], y[3]);
-        if (__any_sync(0xffffffffu, top0 > m[0] + kSlack || top1 > m[1] + kSlack)) {
+        if (__any_sync(0xffffffffu, top0 > m[0] + kTopWeight || top1 > m[1] + kTopWeight)) {
             float top[2] = {top0, top1};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], o));
-                const float now = fmaxf(m[h], top[h]), f = fast_exp2(m[h] - now);
+                const float now = fmaxf(m[h], top[h] - kHeadroom), f = fast_exp2(m[h] - now);
                 m[h] = now;
                 l[h] *= f;
 #pragma unroll
@@ -379,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
         float pr[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) pr[c] = fast_exp2(y[c] - m[c & 1]);
-        const float inv = __frcp_rn(vs);
+        const float inv = __frcp_rn(vs) * kSumUnit;
         l[0] = fmaf(pr[0] + pr[2], inv, l[0]);
         l[1] = fmaf(pr[1] + pr[3], inv, l[1]);
         const uint32_t b0 = movmatrix_t(pack_h2(pr[0], pr[1])), b1 = movmatrix_t(pack_h2(pr[2], pr[3]));
@@ -427,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
                     const int hq = 2 * t + h;
                     if (hq >= p.group) continue;
                     const size_t cell = (size_t)b * p.num_q_heads + head * p.group + hq;
-                    const float f = l[h] == 0.0f ? 0.0f : __frcp_rn(l[h]);
+                    const float f = output_factor(l[h]);
                     uint16_t* out = static_cast<uint16_t*>(p.out) + cell * kHeadDim;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {

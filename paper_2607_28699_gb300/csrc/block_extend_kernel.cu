@@ -12,7 +12,7 @@
 // the other's; warps 8-11: codes to fp16 operands, two stages; warp 12: the MMAs; warp 13: block table, scales
 // and the codes' way to shared memory by TMA (read with ordinary loads in rows of 64 bytes, the shape in which
 // the operands are written without bank conflicts, they cost the MMAs' operand fetch a third of its time).
-// A softmax thread moves its running maximum (and its row of O) only when a logit passes it by 2^8.
+// A softmax thread moves its frame m (and its row of O) only when a weight would pass 2^15.
 //
 // GB300, 28 query / 4 KV heads: 4096 tokens at the end of 32k, int8 codes, fp16: 1209 us, 1491 TFLOP/s (0.78 of the
 // measured cuBLAS bf16 rate); an 8k prompt from e4m3, bf16: 358 us, 1345 TFLOP/s (11 us of a CTA's 65 pass
@@ -43,7 +43,6 @@ constexpr int kBlock = kOperand / 2;
 constexpr int kCodes = kTile * kHeadDim;         // bytes of a context tile's keys, or values
 constexpr int kMetaStages = 4;
 constexpr float kNoMax = -1e30f;
-constexpr float kSlack = 8.0f;
 constexpr uint32_t kTmemColumns = 512, kOutColumn = 256;   // S (and P) of tile t at 128 t, O at 256 + 128 t
 
 struct Meta {   // of a context tile's pages
@@ -230,7 +229,7 @@ __device__ __forceinline__ float first_max(uint32_t s_at, const Meta& meta, floa
     return top;
 }
 
-// A row's weights for a context tile under the maximum m: pairs as fp16 in y, their sum (in units of the
+// A row's weights for a context tile in the frame m: pairs as fp16 in y, their sum (in units of the
 // weights p: value scales divided out) returned; top: the tile's largest exponent.  kMask: the row sees the first
 // `sees` keys of the tile only.
 template <bool kMask>
@@ -392,12 +391,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                     const bool masked = least < key0 + kTile;
                     uint32_t y[kTile / 2];
                     float sum;
-                    if (j == 0) m = first_max(s_at, meta, factor, sees);
-                    for (;;) {   // again where a logit passed the maximum by too much: rarely
+                    if (j == 0) m = first_max(s_at, meta, factor, sees) - kHeadroom;
+                    for (;;) {   // again where a logit passed the frame by too much: rarely
                         float top;
                         sum = masked ? weights<true>(s_at, meta, factor, m, sees, y, top) : weights<false>(s_at, meta, factor, m, sees, y, top);
-                        if (!__any_sync(0xffffffffu, top > m + kSlack)) break;
-                        const float now = fmaxf(m, top), f = fast_exp2(m - now);
+                        if (!__any_sync(0xffffffffu, top > m + kTopWeight)) break;
+                        const float now = fmaxf(m, top - kHeadroom), f = fast_exp2(m - now);
                         m = now;
                         l *= f;
                         if (j == 0) continue;
@@ -428,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
         const size_t cell = (size_t)mine.token * p.num_q_heads + head * p.group + mine.hq;
         const size_t part = (size_t)blockIdx.z * p.n_tok * p.num_q_heads + cell;
         if (ok && n > 0 && t < tiles_q) {
-            const float f = l == 0.0f ? 0.0f : __frcp_rn(l);
+            const float f = output_factor(l);
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 uint32_t x[32];
@@ -628,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                         const float of = no_values ? kNoValueScale : vs;
                         meta.ks[lane] = ks * p.scale_log2;
                         meta.bias[lane] = outside ? -INFINITY : log2f(of);
-                        meta.inv[lane] = __frcp_rn(of);
+                        meta.inv[lane] = __frcp_rn(of) * kSumUnit;
                         meta.tokens[0][lane] = tokens;
                         meta.tokens[1][lane] = no_values ? 0 : tokens;
                         if (lost) {
