@@ -173,7 +173,7 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
         position[j] = t;
         if (mine[j]) {
             raw[j] = load_raw(rows + 2 * ((size_t)row * p.x_stride[side]), at.a, at.b);
-            if (rot && p.positions) position[j] = load_dep(p.positions + row);
+            if (p.rotary_dim && p.positions) position[j] = load_dep(p.positions + row);
         }
     }
     // Rows are rotated for their amax and again for their codes: kept as fp32 they would take the registers of a
@@ -186,7 +186,7 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
     uint32_t amax = 0;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
-        if (rot && mine[j] && (position[j] < 0 || position[j] >= p.num_positions)) {
+        if (p.rotary_dim && mine[j] && (position[j] < 0 || position[j] >= p.num_positions)) {
             report(p, WC_DEV_BAD_POSITION);
             mine[j] = false;
         }
