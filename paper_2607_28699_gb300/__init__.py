@@ -500,10 +500,13 @@ class BlockDesc:
         return self._c
 
 
+_CODE_TYPE = {torch.int8: CODE_INT8, torch.uint8: CODE_E4M3, torch.float8_e4m3fn: CODE_E4M3}
+
+
 @dataclass(frozen=True)
 class BlockCache:
-    """One layer's block-scaled cache tensors (layout in ``include/witcert.h``); without scales
-    (None) a cache of raw fp8 codes, such as a ``LayerCache``'s of the fp8 scheme."""
+    """One layer's block-scaled cache tensors (layout in ``include/witcert.h``): codes int8, or uint8 or float8_e4m3fn for
+    ``CODE_E4M3``; without scales (None) a cache of raw fp8 codes, such as a ``LayerCache``'s of the fp8 scheme."""
     k_codes: torch.Tensor
     v_codes: torch.Tensor
     k_scale: Optional[torch.Tensor]
@@ -518,6 +521,8 @@ class BlockCache:
             if t is not None and (t.dtype != torch.float32 or t.numel() != blocks or not t.is_contiguous()):
                 raise ValueError("the cache's scales must be contiguous float32 [num_pages, num_kv_heads]")
         object.__setattr__(self, "blocks", blocks)
+        k, v = (_CODE_TYPE.get(t.dtype) for t in (self.k_codes, self.v_codes))
+        object.__setattr__(self, "code", k if k == v else None)
 
     @staticmethod
     def empty(desc: BlockDesc, device="cuda"):
@@ -574,6 +579,8 @@ def _ints(t: torch.Tensor, n: int, name: str):
 def _block_cache(desc: BlockDesc, c: BlockCache):
     if c.blocks != desc.num_pages * desc.num_kv_heads:
         raise ValueError("the cache does not have the descriptor's shape")
+    if c.code != desc.code:
+        raise ValueError(f"the cache's codes ({c.k_codes.dtype}, {c.v_codes.dtype}) are not the descriptor's (code {desc.code})")
     ks, vs = c.k_scale, c.v_scale
     return (c.k_codes.data_ptr(), c.v_codes.data_ptr(), None if ks is None else ks.data_ptr(),
             None if vs is None else vs.data_ptr())
