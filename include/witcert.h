@@ -79,7 +79,9 @@ enum {
     WC_DEV_BAD_POSITION = 64u,/* block append: a rotary position outside the tables; the
                                  token is not written, its rotated query rows are 0 */
     WC_DEV_BAD_ROWS = 128u    /* block calls: a sequence's token range [cu[b], cu[b + 1]) is not
-                                 an ascending one within [0, n_tok]; the sequence is skipped */
+                                 an ascending one within [0, n_tok]; the sequence is skipped, and
+                                 what the ones after it get is not defined, nor what rows get that
+                                 theirs overlap (with more than 32 sequences: what any other gets) */
 };
 
 typedef enum {

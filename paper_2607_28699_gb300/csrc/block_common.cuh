@@ -146,7 +146,9 @@ __device__ __forceinline__ uint32_t scaled_bf16(uint32_t w, float by) {
     return pack_h2(f.x * by, f.y * by);
 }
 
-// The sequence whose first[b] is the last one <= x, for ascending first(0) <= x; a warp searches together.
+// The sequence whose first[b] is the last one <= x, for ascending first(0) <= x; a warp searches together.  Where first does
+// not ascend, the last one of those that begin with first(0) and are <= x, so that ranges that cannot be do not hide the ones
+// before them (of up to 32).
 template <typename F>
 __device__ __forceinline__ int warp_find_last(int n, long long x, F first) {
     int lo = 0;
@@ -154,7 +156,7 @@ __device__ __forceinline__ int warp_find_last(int n, long long x, F first) {
         const int step = (len + 31) / 32;
         const int at = lo + (threadIdx.x & 31) * step;
         const bool le = at < lo + len && first(at) <= x;
-        const int k = __popc(__ballot_sync(0xffffffffu, le)) - 1;   // lane 0 holds by assumption
+        const int k = __clz(__brev(~__ballot_sync(0xffffffffu, le))) - 1;   // lane 0 holds by assumption
         const int next = lo + max(k, 0) * step;
         len = min(step, lo + len - next);
         lo = next;
