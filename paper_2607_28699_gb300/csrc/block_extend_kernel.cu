@@ -380,6 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
             const bool live = thread < rows;
             const int seen = live ? keys_seen(p, w, w.row0 + t * kTile + thread) : 0;
             const int least = __reduce_min_sync(0xffffffffu, live ? seen : w.ctx);   // of the warp's rows
+            if (!live) m = -kNoMax;   // rows past the last (zeros): nothing passes their frame, so they hold no warp up
             const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + t * kTile + lanes, o_at = tmem + kOutColumn + t * kTile + lanes;
             if (t < tiles_q) {
                 for (int j = 0; j < n && ok; ++j) {
@@ -391,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                     const bool masked = least < key0 + kTile;
                     uint32_t y[kTile / 2];
                     float sum;
-                    if (j == 0) m = first_max(s_at, meta, factor, sees) - kHeadroom;
+                    if (j == 0) m = fmaxf(m, first_max(s_at, meta, factor, sees) - kHeadroom);
                     for (;;) {   // again where a logit passed the frame by too much: rarely
                         float top;
                         sum = masked ? weights<true>(s_at, meta, factor, m, sees, y, top) : weights<false>(s_at, meta, factor, m, sees, y, top);
