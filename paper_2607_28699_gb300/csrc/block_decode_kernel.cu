@@ -35,7 +35,7 @@ constexpr int kPageBytes = kPage * kHeadDim;           // one head's page of key
 constexpr int kStageBytes = 2 * kPageBytes;
 constexpr int kRow = kHeadDim + 4;                     // floats of a merge row in shared memory
 constexpr int kMinPages = 1;                           // per warp, before a launch takes more CTAs
-constexpr float kNoMax = -1e30f;                       // the frame before the first logit
+constexpr float kNoMax = -3e38f;                       // the frame before the first logit
 
 struct DecodeArgs {
     BlockAttentionParams p;

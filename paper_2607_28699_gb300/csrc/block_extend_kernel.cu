@@ -42,7 +42,7 @@ constexpr int kOperand = kTile * kHeadDim * 2;   // bytes of a [128][128] fp16 o
 constexpr int kBlock = kOperand / 2;
 constexpr int kCodes = kTile * kHeadDim;         // bytes of a context tile's keys, or values
 constexpr int kMetaStages = 4;
-constexpr float kNoMax = -1e30f;
+constexpr float kNoMax = -3e38f;
 constexpr uint32_t kTmemColumns = 512, kOutColumn = 256;   // S (and P) of tile t at 128 t, O at 256 + 128 t
 
 struct Meta {   // of a context tile's pages
