@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
             l[0] = l[1] = 0.0f;
             seg = first + i;
         }
-        if (ok && !mbar_wait_bounded(&s.bars[warp][i % kStages], (i / kStages) & 1)) {
+        if (ok && !__all_sync(0xffffffffu, mbar_wait_bounded(&s.bars[warp][i % kStages], (i / kStages) & 1))) {
             if (lane == 0) atomicOr(p.status, WC_DEV_TIMEOUT);
             ok = false;
         }

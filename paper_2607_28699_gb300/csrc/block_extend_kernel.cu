@@ -142,7 +142,8 @@ __device__ __forceinline__ void copy_async(void* dst, const void* src, int bytes
 }
 __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Bounded wait (about two seconds); once one gives up, all do.
+// Bounded wait (about two seconds); once one gives up, all do.  A warp waits together and gets one answer: a lane that saw the
+// barrier complete just as the others gave up would go on without them.
 __device__ __forceinline__ bool wait(Shared& s, uint64_t* bar, uint32_t parity) {
     const uint32_t at = smem_addr(bar);
     uint64_t since = 0;
@@ -152,17 +153,16 @@ __device__ __forceinline__ bool wait(Shared& s, uint64_t* bar, uint32_t parity) 
                      : "=r"(ok)
                      : "r"(at), "r"(parity)
                      : "memory");
-        if (ok) return true;
+        if (__all_sync(0xffffffffu, ok)) return true;
         if (i % 64 == 0) {
             uint64_t now;
             asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
             if (since == 0) since = now;
-            if (*reinterpret_cast<volatile int*>(&s.abandoned)) return false;
-            if (now - since > 2000000000ull) break;
+            const bool over = now - since > 2000000000ull;
+            if (over) *reinterpret_cast<volatile int*>(&s.abandoned) = 1;
+            if (__any_sync(0xffffffffu, over || *reinterpret_cast<volatile int*>(&s.abandoned))) return false;
         }
     }
-    *reinterpret_cast<volatile int*>(&s.abandoned) = 1;
-    return false;
 }
 
 // ---- work ---------------------------------------------------------------------------------------
