@@ -649,10 +649,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_extend_kernel(const __grid_
                 vs = next_vs;
                 next = after;
             }
-            // copies in flight end before the CTA does (bounded): those of the last tile are all waited for by the conversion
-            if (!ok)
-                for (int side = 0; side < 2; ++side)
-                    for (int parity = 0; parity < 2; ++parity) (void)mbar_wait_bounded<64>(&s.codes_full[side], parity);
+            // copies in flight end before the CTA does (bounded): the last tile's, or whichever there are where a wait gave up; the
+            // conversion may have given up since the last one was issued
+            for (int side = 0; side < 2; ++side) {
+                if (ok) (void)mbar_wait_bounded<64>(&s.codes_full[side], (n - 1) & 1);
+                else for (int parity = 0; parity < 2; ++parity) (void)mbar_wait_bounded<64>(&s.codes_full[side], parity);
+            }
         }
     }
     __syncthreads();
