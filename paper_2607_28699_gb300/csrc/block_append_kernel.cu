@@ -223,7 +223,7 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 uint32_t lo, hi;
-                codes4_to_h2<kCode>(word_at(c, k), lo, hi);
+                codes4_to_h2<kCode>(word_of(c, k), lo, hi);
                 const float2 f = h2_to_float2(lo), g = h2_to_float2(hi);
                 out[k] = finite ? encode4<kCode>(__fmul_rn(f.x, ratio), __fmul_rn(f.y, ratio), __fmul_rn(g.x, ratio), __fmul_rn(g.y, ratio)) : 0u;
             }

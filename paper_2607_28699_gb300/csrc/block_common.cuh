@@ -79,8 +79,6 @@ __device__ __forceinline__ uint32_t float2_to_act2(float lo, float hi) {
     }
 }
 
-__device__ __forceinline__ uint32_t word_at(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-
 // Four codes of a word as two exact half2 (codes 0, 1 and 2, 3).
 template <int kCode>
 __device__ __forceinline__ void codes4_to_h2(uint32_t w, uint32_t& lo, uint32_t& hi) {

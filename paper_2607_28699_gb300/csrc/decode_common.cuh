@@ -97,10 +97,6 @@ __device__ __forceinline__ uint32_t u8x2_minus(uint32_t w_xor80, uint32_t sel, u
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) {
-    return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
-}
-
 // Transpose of an 8x8 b16 matrix held in the mma fragment layout.
 __device__ __forceinline__ uint32_t movmatrix_t(uint32_t x) {
     uint32_t y;

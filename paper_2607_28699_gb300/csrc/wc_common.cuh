@@ -162,6 +162,10 @@ __device__ __forceinline__ uint32_t e4m3x2_to_h2(uint32_t w16) {
     return d;
 }
 
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) {
+    return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+}
+
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
     __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
