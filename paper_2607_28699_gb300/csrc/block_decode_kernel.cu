@@ -14,8 +14,8 @@
 // that reaches over several leave partial results, and the last of them to arrive merges these
 // (in the order of the pages, so the result does not depend on which one it is).
 //
-// GB300, 4 KV heads of 7 query heads: 32 sequences of 4k to 32k 107 us (5.65 TB/s, 0.83 of the measured copy rate: the
-// page loop reads 7 TB/s, the rest is the first pages' latency and the merges), 16 of 4k to 8k 33 us, one of 32k 21 us
+// GB300, 4 KV heads of 7 query heads: 32 sequences of 4k to 32k 106 us (5.7 TB/s, 0.84 of the measured copy rate: the
+// page loop reads 7 TB/s, the rest is the first pages' latency and the merges), 16 of 4k to 8k 33 us, one of 32k 20 us
 // (6 us page loop at the copy rate; launch and block table before it, merges in the CTA and over 38 CTAs after it).
 // 16 warps on one CTA an SM (with three pages in flight each: 111 / 35 / 20.5 us; 8 warps on two CTAs 110 / 35 / 26, twice the
 // partial results; on one 131 / 37 / 23); several shares per SM, taken as SMs come free, 121 / 45 / 41 (each has its own

@@ -13,10 +13,12 @@
 // and the codes' way to shared memory by TMA (read with ordinary loads in rows of 64 bytes, the shape in which
 // the operands are written without bank conflicts, they cost the MMAs' operand fetch a third of its time).
 // A softmax thread moves its frame m (and its row of O) only when a weight would pass 2^15.
+// Values that are NaN count as 0 in the second product wherever a row may not see them (its weight of 0 would not silence
+// them); the rows that do see them get theirs at the end.
 //
-// GB300, 28 query / 4 KV heads: 4096 tokens at the end of 32k, int8 codes, fp16: 1209 us, 1491 TFLOP/s (0.78 of the
-// measured cuBLAS bf16 rate); an 8k prompt from e4m3, bf16: 358 us, 1345 TFLOP/s (11 us of a CTA's 65 pass
-// before its first and after its last product); 16 sequences of 5 drafted tokens at 4k to 8k 65 us, where
+// GB300, 28 query / 4 KV heads: 4096 tokens at the end of 32k, int8 codes, fp16: 1208 us, 1493 TFLOP/s (0.79 of the
+// measured cuBLAS bf16 rate); an 8k prompt from e4m3, bf16: 370 us, 1300 TFLOP/s (11 us of a CTA's 65 pass
+// before its first and after its last product); 16 sequences of 5 drafted tokens at 4k to 8k 65.5 us, where
 // one tile of rows leaves its softmax (1450 cycles a step) and its products (1100) to follow each other.  A step of two
 // tiles costs 3050 cycles against the MMAs' 2050: what the issuing warp waits for is not hidden, as few MMAs queue.
 // Tried and slower: a warp per tile issuing MMAs (1480 us, taking turns by a barrier 1391), the copies'
