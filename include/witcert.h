@@ -565,7 +565,9 @@ size_t wc_block_workspace_size(const wc_block_desc* desc, int32_t batch, int32_t
  *   out[b][hq][:] = sum_t p_t v^_t,  p = softmax_t(softmax_scale q . k^_t),  t < ctx_lens[b]
  *   lse[b][hq]    = log sum_t e^(softmax_scale q . k^_t)
  * fp32 sums and softmax statistics, out rounded once.  A sequence with no context gets out = 0 and
- * lse = -inf.  What the pages hold past the context is never used.
+ * lse = -inf.  What the pages hold past the context is never used.  Logits (softmax_scale q . k) are below
+ * 2^22 in magnitude: fp32 holds differences of larger ones to 1/2 and worse (in the extend's form of the
+ * products, and with more than 8 query heads per KV head, such a row can lose its output).
  *   q            [batch][Hq][128] act_type, rotated; q_stride elements from one token to the next
  *   out          [batch][Hq][128] act_type; lse [batch][Hq] fp32 or NULL
  *   k_scale, v_scale  NULL together: scale 1 (WC_CODE_E4M3 only)

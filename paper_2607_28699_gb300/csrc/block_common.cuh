@@ -106,7 +106,8 @@ constexpr float kLeastValueScale = 0x1p-100f, kNoValueScale = 0x1p-80f;
 
 // Weights 2^(y - m) are rounded to fp16 for the second product.  The frame m is put kHeadroom below the largest y, and moves
 // when one passes it by kTopWeight: the largest weight lies in [2^7, 2^15], and others keep all their bits down to 2^-21
-// of it, some to 2^-32 (from 1 on: 2^-14 and 2^-25, and what a sharp head gives to many tokens in all was lost below).
+// of it, some to 2^-32 (from 1 on: 2^-14 and 2^-25, and what a sharp head gives to many tokens in all was lost below).  2^15
+// leaves fp16's range a factor of 2 for what fp32 rounds off exponents: those of logits up to 2^22.
 constexpr float kHeadroom = 7.0f, kTopWeight = 15.0f;
 // The sum of weights l is kept times 2^-10: with value scales from 2^-100 on and 2^20 tokens it stays within fp32's range, and
 // so do the reciprocals of the largest scales.

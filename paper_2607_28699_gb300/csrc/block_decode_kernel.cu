@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_decode_kernel(const __grid_
             if (trow + 2 >= tokens) y[2] = y[3] = -INFINITY;
         }
         const float top0 = fmaxf(y[0], y[2]), top1 = fmaxf(y[1], y[3]);
-        if (__any_sync(0xffffffffu, top0 > m[0] + kTopWeight || top1 > m[1] + kTopWeight)) {
+        if (__any_sync(0xffffffffu, top0 - m[0] > kTopWeight || top1 - m[1] > kTopWeight)) {
             float top[2] = {top0, top1};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
