@@ -80,10 +80,36 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
     }
 }
 
+// A warp's page task, KV head and side: (task, head, side), side fastest.  group: of its CTA among those of pages.
+struct PageWork {
+    unsigned task, rest;
+    __device__ __forceinline__ PageWork(const BlockAppendParams& p, unsigned group, unsigned warp) {
+        const unsigned t = group * kWarps + warp, per = 2 * p.num_kv_heads;
+        task = t / per;
+        rest = t - task * per;
+    }
+};
+
+enum class Norm { kNone, kUsual, kWide };   // kWide: factors in 64 bits
+template <int kCode, bool kBf16, bool kHalfLayout, Norm kOf>
+__device__ __forceinline__ void append_page(const BlockAppendParams& p, int task, int head, int side);
+
+// A warp's page anew, with factors in 64 bits.  A function of its own, which finds its task again: usual pages have no register for
+// what it takes (a 32k prompt with norms 114.8 us as without it; inlined, or with the task passed on, 117.6).
+template <int kCode, bool kBf16, bool kHalfLayout>
+__device__ __noinline__ void append_wide_page(const BlockAppendParams& p) {
+    unsigned cta, thread;   // read again, not kept
+    asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(cta));
+    asm volatile("mov.u32 %0, %%tid.x;" : "=r"(thread));
+    const PageWork w(p, cta / (unsigned)p.page_stride, __shfl_sync(0xffffffffu, thread >> 5, 0));
+    append_page<kCode, kBf16, kHalfLayout, Norm::kWide>(p, (int)w.task, w.rest >> 1, w.rest & 1);
+}
+
 // One warp: the new rows of one page and KV head, keys (side 0) or values.  A lane holds its channels of every
 // fourth row, so the page's amax is one warp reduction and the rows are read once.
-template <int kCode, bool kBf16, bool kHalfLayout, bool kNorm>
+template <int kCode, bool kBf16, bool kHalfLayout, Norm kOf>
 __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task, int head, int side) {
+    constexpr bool kNorm = kOf != Norm::kNone;
     const int lane = threadIdx.x & 31, sub = lane >> 3, i = lane & 7;
     // page tasks of sequence b: cu[b] / 16 + 2 b on, two more than its whole pages (n rows reach
     // into at most n / 16 + 2)
@@ -157,7 +183,7 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
     // of a third of the warps, or of half as fp32.
     uint32_t mine = 0;             // bit j: step j has a row of this lane
     float most = 0.0f;
-    float factors = 0.0f;          // lane i: of step i
+    float factors = 1.0f;          // lane i: of step i
 #pragma unroll (kNorm ? 1 : kSteps)
     for (int j = 0; j < kSteps; ++j) {
         Raw raw = next;
@@ -166,7 +192,8 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
         float factor = 1.0f;
         if constexpr (kNorm) {
             if (normed) {
-                factor = norm_factor<kBf16>(raw, p.norm_eps);
+                if constexpr (kOf == Norm::kWide) factor = wide_factor<kBf16>(raw, p.norm_eps);
+                else factor = norm_factor<kBf16>(raw, p.norm_eps);
                 if (i == j) factors = factor;
                 forget(raw);
             }
@@ -184,6 +211,9 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
 #pragma unroll
             for (int e = 0; e < 8; e += 2) most = most_of(most, y[e], y[e + 1]);
         }
+    }
+    if constexpr (kOf == Norm::kUsual) {
+        if (__any_sync(0xffffffffu, far_factor(factors))) return append_wide_page<kCode, kBf16, kHalfLayout>(p);
     }
     const uint32_t amax = __reduce_max_sync(0xffffffffu, __float_as_uint(most));   // bits order like the magnitudes, NaN above all
     const uint32_t now = max(scale_bits<kCode>(amax), had);
@@ -301,14 +331,13 @@ __global__ void __launch_bounds__(kThreads, kNorm ? 7 : 8) block_append_kernel(c
     // CTAs of pages lie among those of queries: theirs is a chain of loads, which the others' bytes hide
     const unsigned group = blockIdx.x / (unsigned)p.page_stride, member = blockIdx.x - group * p.page_stride;
     if (member == 0 && group < (unsigned)p.page_ctas) {
-        const unsigned t = group * kWarps + warp, per = 2 * p.num_kv_heads, task = t / per;   // (page task, head, side), side fastest
-        const unsigned rest = t - task * per;
-        if (task == (unsigned)p.page_tasks && rest == 0) {   // one warp more reports the sequences that the others skip
+        const PageWork w(p, group, warp);
+        if (w.task == (unsigned)p.page_tasks && w.rest == 0) {   // one warp more reports the sequences that the others skip
             Sequence s;
             for (int b = threadIdx.x & 31; b < p.batch; b += 32) sequence<true>(p, b, s);
         }
-        if (task >= (unsigned)p.page_tasks) return;
-        append_page<kCode, kBf16, kHalfLayout, kNorm>(p, (int)task, rest >> 1, rest & 1);
+        if (w.task >= (unsigned)p.page_tasks) return;
+        append_page<kCode, kBf16, kHalfLayout, kNorm ? Norm::kUsual : Norm::kNone>(p, (int)w.task, w.rest >> 1, w.rest & 1);
     } else {
         const unsigned t = (blockIdx.x - min(group + 1, (unsigned)p.page_ctas)) * kWarps + warp;
         const unsigned per = (p.num_q_heads + p.q_heads - 1) / p.q_heads, row = t / per;

@@ -157,23 +157,43 @@ __device__ __forceinline__ TwoFloats sum_of_squares(const Raw& raw) {
     return s;
 }
 
-// 1 / sqrt(sum / 128 + eps), rounded once (but for one in a million): one Newton step on the library's answer, the residual
-// 1 - r^2 v in two floats.
-__device__ __forceinline__ float inverse_root(TwoFloats sum, float eps) {
-    TwoFloats v = {sum.hi * (1.0f / kHeadDim), sum.lo * (1.0f / kHeadDim)};
-    add_exactly(v, eps);
-    float r;   // of a normal number: eps is
+// 1 / sqrt(v), rounded once (but for one in a million): one Newton step on the library's answer, the residual 1 - r^2 v in two
+// floats.  For v from 2^-60 to 2^80: what the residual is made of stays above fp32's least numbers.
+__device__ __forceinline__ float inverse_root(TwoFloats v) {
+    float r;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v.hi));
     const float q = __fmul_rn(r, r), q_lo = fmaf(r, r, -q), t = __fmul_rn(q, v.hi), t_lo = fmaf(q, v.hi, -t);
     const float rest = fmaf(-q, v.lo, fmaf(-q_lo, v.hi, __fsub_rn(__fsub_rn(1.0f, t), t_lo)));
     return __fadd_rn(r, __fmul_rn(__fmul_rn(0.5f, r), rest));
 }
 
-// The factor of a row (a warp takes four together): NaN for one with infinities or NaN, or with a sum of squares past fp32's
-// range (bf16 values from 2^60 on).
+// The factor of a row (a warp takes four together), 1 / sqrt(mean + eps): NaN for one with infinities or NaN, or with a sum of
+// squares past fp32's range (bf16 values from 2^60 on).
 template <bool kBf16>
 __device__ __forceinline__ float norm_factor(const Raw& raw, float eps) {
-    return inverse_root(sum_of_squares<kBf16>(raw), eps);
+    const TwoFloats sum = sum_of_squares<kBf16>(raw);
+    TwoFloats v = {sum.hi * (1.0f / kHeadDim), sum.lo * (1.0f / kHeadDim)};
+    add_exactly(v, eps);
+    return inverse_root(v);
+}
+
+// Whether a factor says that mean + eps is so far from 1 that the two floats lost what they are for, or passed the range on the way
+// (they hold up to three times the largest square: NaN): wide_factor has those rows'.
+__device__ __forceinline__ bool far_factor(float r) { return !(r >= 0x1p-40f && r <= 0x1p30f); }
+
+// The same in 64 bits, for any row.
+template <bool kBf16>
+__device__ __forceinline__ float wide_factor(const Raw& raw, float eps) {
+    const uint32_t w[8] = {raw.a.x, raw.a.y, raw.a.z, raw.a.w, raw.b.x, raw.b.y, raw.b.z, raw.b.w};
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float2 f = act2_to_float2<kBf16>(w[j]);
+        s = fma((double)f.x, (double)f.x, fma((double)f.y, (double)f.y, s));
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return (float)s < INFINITY ? (float)rsqrt(s * (1.0 / kHeadDim) + (double)eps) : NAN;
 }
 
 // y = (y r) w, each product rounded; a, b the lane's chunks of the weights.
