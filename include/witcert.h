@@ -560,7 +560,8 @@ wc_status wc_block_append(const wc_block_desc* desc, int32_t act_type,
  * codes do not depend on the order of a sum.  Queries: in fp32 (to 2^-20 of the row's largest), rounded once to
  * act_type.  A row with infinities or NaN, or whose sum of squares passes fp32's range (bf16 values from 2^60 on),
  * becomes NaN (rows of k: the page's scale is NaN, as above).
- *   k_norm, q_norm  [128] fp32, device, 16-byte aligned, the same for every head; NULL: rows are not normed
+ *   k_norm, q_norm  [128] fp32, device, 16-byte aligned, the same for every head; NULL: rows are not normed, and
+ *                   are bit for bit wc_block_append's
  *   norm_eps        finite, >= 2^-126; not looked at where both are NULL
  * Other arguments as wc_block_append.
  */
@@ -581,7 +582,7 @@ wc_status wc_block_append_norm(const wc_block_desc* desc, int32_t act_type,
  *   q, q_out     [n_tok][num_q_heads][128] act_type and out_type, token strides in elements as in
  *                wc_block_append; both NULL: no queries.  k, k_out likewise.  An output may be its input (same
  *                type and stride: in place, of a packed projection too); no other overlap
- *   q_norm, k_norm  as above; NULL: the rows are only rotated
+ *   q_norm, k_norm  as above; NULL: the rows are only rotated, bit for bit as the queries of wc_block_append
  *   rope_layout, rotary_dim  as in wc_block_desc; positions [n_tok] int32, cos_table, sin_table
  *                [num_positions][rotary_dim / 2]: NULL if rotary_dim is 0
  *   dev_status   optional device uint32: WC_DEV_BAD_POSITION (the token's rows are zeros)

@@ -291,36 +291,28 @@ __device__ __forceinline__ void rotate_queries(const BlockAppendParams& p, int r
     for (int part = 0; part < 2; ++part)
         if (at.rotated(part) && !bad) load_trig(p.cos_table, p.sin_table, (size_t)position * (rot >> 1) + at.first_pair(part), trig[part]);
     const float* weight = kNorm && !bad ? p.q_norm : nullptr;   // a bad row's are zeros
-    for (int h0 = head0; h0 < end; h0 += 4 * kAhead) {
+    auto rows = [&](auto with) {
+        constexpr bool normed = decltype(with)::value;
+        for (int h0 = head0; h0 < end; h0 += 4 * kAhead) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            float factor = 1.0f;
-            if constexpr (kNorm) {
-                if (weight) factor = quick_factor<kBf16>(raw[j], p.norm_eps);   // the warp together
+            for (int j = 0; j < kAhead; ++j) {
+                float factor = 1.0f;
+                if constexpr (normed) factor = quick_factor<kBf16>(raw[j], p.norm_eps);   // the warp together
+                if (bad) raw[j] = {};
+                uint4 a, b;
+                finished_row<normed, kBf16, kBf16>(raw[j], at, weight, factor, !bad, trig, a, b);
+                raw[j] = load(h0 + 4 * (j + kAhead));
+                if (h0 + 4 * j + sub >= end) continue;
+                uint4* out = reinterpret_cast<uint4*>(dst + (h0 + 4 * j) * (2 * kHeadDim));
+                out[at.a] = a;
+                out[at.b] = b;
             }
-            if (bad) raw[j] = {};
-            uint4 a, b;
-            if constexpr (kNorm) {
-                normed_row<kBf16, kBf16>(raw[j], at, weight, factor, !bad, trig, a, b);
-            } else {   // products rounded one by one
-                uint2 wa[2], wb[2];
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    float y[8];
-                    unpack<kBf16, kHalfLayout>(raw[j], part, y);
-                    if (at.rotated(part) && !bad) rotate<kHalfLayout>(trig[part], y);
-                    place<kHalfLayout>(wa, wb, part, float4_to_act<kBf16>(y), float4_to_act<kBf16>(y + 4));
-                }
-                a = make_uint4(wa[0].x, wa[0].y, wa[1].x, wa[1].y);
-                b = make_uint4(wb[0].x, wb[0].y, wb[1].x, wb[1].y);
-            }
-            raw[j] = load(h0 + 4 * (j + kAhead));
-            if (h0 + 4 * j + sub >= end) continue;
-            uint4* out = reinterpret_cast<uint4*>(dst + (h0 + 4 * j) * (2 * kHeadDim));
-            out[at.a] = a;
-            out[at.b] = b;
         }
+    };
+    if constexpr (kNorm) {
+        if (weight) return rows(std::true_type{});
     }
+    rows(std::false_type{});
 }
 
 template <int kCode, bool kBf16, bool kHalfLayout, bool kNorm>

@@ -256,17 +256,22 @@ __device__ __forceinline__ void quick_rotate(const Trig& t, float (&y)[8]) {
     }
 }
 
-// A row of a lane, normed (weight not null) and rotated (turn), as 16-bit words of its chunks.
-template <bool kBf16, bool kOutBf16, bool kHalfLayout>
-__device__ __forceinline__ void normed_row(const Raw& raw, const Chunks<kHalfLayout>& at, const float* weight, float r, bool turn, const Trig (&trig)[2],
+// A row of a lane, normed (kNormed) and rotated (turn), as 16-bit words of its chunks.  Rows that are not normed are rotated with
+// every product rounded, whatever the call.
+template <bool kNormed, bool kBf16, bool kOutBf16, bool kHalfLayout>
+__device__ __forceinline__ void finished_row(const Raw& raw, const Chunks<kHalfLayout>& at, const float* weight, float r, bool turn, const Trig (&trig)[2],
                                            uint4& a, uint4& b) {
     uint2 wa[2], wb[2];
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
         float y[8];
         unpack<kBf16, kHalfLayout>(raw, part, y);
-        if (weight) scale_part<kHalfLayout>(weight, at.a, at.b, part, r, y);
-        if (turn && at.rotated(part)) quick_rotate<kHalfLayout>(trig[part], y);
+        if constexpr (kNormed) {
+            scale_part<kHalfLayout>(weight, at.a, at.b, part, r, y);
+            if (turn && at.rotated(part)) quick_rotate<kHalfLayout>(trig[part], y);
+        } else {
+            if (turn && at.rotated(part)) rotate<kHalfLayout>(trig[part], y);
+        }
         place<kHalfLayout>(wa, wb, part, float4_to_act<kOutBf16>(y), float4_to_act<kOutBf16>(y + 4));
     }
     a = make_uint4(wa[0].x, wa[0].y, wa[1].x, wa[1].y);

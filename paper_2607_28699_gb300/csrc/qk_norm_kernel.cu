@@ -53,10 +53,10 @@ __global__ void __launch_bounds__(kThreads, 8) qk_norm_rotate_kernel(const __gri
             const bool key = s >= q_steps;
             const int step = key ? s - q_steps : s;
             const float* weight = bad ? nullptr : key ? p.weight[1] : p.weight[0];   // a bad row's are zeros
-            const float factor = weight ? quick_factor<kBf16>(raw[j], p.eps) : 1.0f;   // the warp together
             if (bad) raw[j] = {};
             uint4 a, b;
-            normed_row<kBf16, kOutBf16>(raw[j], at, weight, factor, !bad, trig, a, b);
+            if (weight) finished_row<true, kBf16, kOutBf16>(raw[j], at, weight, quick_factor<kBf16>(raw[j], p.eps), true, trig, a, b);
+            else finished_row<false, kBf16, kOutBf16>(raw[j], at, nullptr, 1.0f, !bad, trig, a, b);
             raw[j] = load(s + kAhead);
             if (s >= end || 4 * step + sub >= (key ? p.heads[1] : p.heads[0])) continue;
             uint4* out = reinterpret_cast<uint4*>((key ? k_dst : q_dst) + step * (8 * kHeadDim));
