@@ -80,13 +80,16 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
     }
 }
 
-// A warp's page task, KV head and side: (task, head, side), side fastest.  group: of its CTA among those of pages.
+// A warp's page task, KV head and side: (task, head, side) of the launch's heads, side fastest.  group: of its CTA among those of pages.
 struct PageWork {
-    unsigned task, rest;
+    unsigned task;
+    int head, side;
     __device__ __forceinline__ PageWork(const BlockAppendParams& p, unsigned group, unsigned warp) {
-        const unsigned t = group * kWarps + warp, per = 2 * p.num_kv_heads;
+        const unsigned t = group * kWarps + warp, per = 2 * p.page_heads;
         task = t / per;
-        rest = t - task * per;
+        const unsigned rest = t - task * per;
+        head = p.page_head0 + (int)(rest >> 1);
+        side = rest & 1;
     }
 };
 
@@ -102,7 +105,7 @@ __device__ __noinline__ void append_wide_page(const BlockAppendParams& p) {
     asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(cta));
     asm volatile("mov.u32 %0, %%tid.x;" : "=r"(thread));
     const PageWork w(p, cta / (unsigned)p.page_stride, __shfl_sync(0xffffffffu, thread >> 5, 0));
-    append_page<kCode, kBf16, kHalfLayout, Norm::kWide>(p, (int)w.task, w.rest >> 1, w.rest & 1);
+    append_page<kCode, kBf16, kHalfLayout, Norm::kWide>(p, (int)w.task, w.head, w.side);
 }
 
 // One warp: the new rows of one page and KV head, keys (side 0) or values.  A lane holds its channels of every
@@ -324,12 +327,12 @@ __global__ void __launch_bounds__(kThreads, kNorm ? 7 : 8) block_append_kernel(c
     const unsigned group = blockIdx.x / (unsigned)p.page_stride, member = blockIdx.x - group * p.page_stride;
     if (member == 0 && group < (unsigned)p.page_ctas) {
         const PageWork w(p, group, warp);
-        if (w.task == (unsigned)p.page_tasks && w.rest == 0) {   // one warp more reports the sequences that the others skip
+        if (w.task == (unsigned)p.page_tasks && w.head == 0 && w.side == 0) {   // one warp more reports the sequences that the others skip
             Sequence s;
             for (int b = threadIdx.x & 31; b < p.batch; b += 32) sequence<true>(p, b, s);
         }
         if (w.task >= (unsigned)p.page_tasks) return;
-        append_page<kCode, kBf16, kHalfLayout, kNorm ? Norm::kUsual : Norm::kNone>(p, (int)w.task, w.rest >> 1, w.rest & 1);
+        append_page<kCode, kBf16, kHalfLayout, kNorm ? Norm::kUsual : Norm::kNone>(p, (int)w.task, w.head, w.side);
     } else {
         const unsigned t = (blockIdx.x - min(group + 1, (unsigned)p.page_ctas)) * kWarps + warp;
         const unsigned per = (p.num_q_heads + p.q_heads - 1) / p.q_heads, row = t / per;
@@ -343,14 +346,14 @@ __global__ void __launch_bounds__(kThreads, kNorm ? 7 : 8) block_append_kernel(c
 cudaError_t launch_block_append(const BlockAppendParams& params, int code, int act, int rope_layout, cudaStream_t stream) {
     BlockAppendParams p = params;
     const long long pages = p.cu_new ? (long long)p.n_tok / kPage + 2LL * p.batch : p.batch;
-    const long long page_ctas = (pages * 2 * p.num_kv_heads + 1 + kWarps - 1) / kWarps;
     // few tokens: eight heads a warp, in parallel; many: 32, behind one read of the angles
     p.q_heads = (long long)p.n_tok * p.num_q_heads >= 16384 ? 32 : 8;
-    const long long q_ctas = p.q ? ((long long)p.n_tok * ((p.num_q_heads + p.q_heads - 1) / p.q_heads) + kWarps - 1) / kWarps : 0;
-    if ((page_ctas + q_ctas) * kWarps > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;   // tasks are counted in 32 bits
+    long long q_ctas = p.q ? ((long long)p.n_tok * ((p.num_q_heads + p.q_heads - 1) / p.q_heads) + kWarps - 1) / kWarps : 0;
+    // A launch counts its warps in 32 bits: where pages times heads are more, it takes some of the heads.
+    const long long most = (0x7FFFFFFFLL - q_ctas * kWarps - 2 * kWarps) / (2 * pages);
+    if (most < 1) return cudaErrorInvalidConfiguration;
     p.page_tasks = (int)pages;
-    p.page_ctas = (int)page_ctas;
-    p.page_stride = (int)((page_ctas + q_ctas) / page_ctas);
+    long long page_ctas = 0;
     auto go = [&](auto code_of, auto bf16, auto half, auto norm) {
         return launch_pdl(block_append_kernel<code_of.value, bf16.value, half.value, norm.value>, dim3((unsigned)(page_ctas + q_ctas)), dim3(kThreads), 0,
                           stream, p);
@@ -363,8 +366,16 @@ cudaError_t launch_block_append(const BlockAppendParams& params, int code, int a
             });
         });
     };
-    if (code == WC_CODE_INT8) return with(std::integral_constant<int, WC_CODE_INT8>{});
-    return with(std::integral_constant<int, WC_CODE_E4M3>{});
+    for (p.page_head0 = 0; p.page_head0 < p.num_kv_heads; p.page_head0 += p.page_heads) {
+        p.page_heads = (int)std::min<long long>(most, p.num_kv_heads - p.page_head0);
+        page_ctas = (pages * 2 * p.page_heads + 1 + kWarps - 1) / kWarps;
+        p.page_ctas = (int)page_ctas;
+        p.page_stride = (int)((page_ctas + q_ctas) / page_ctas);
+        const cudaError_t e = code == WC_CODE_INT8 ? with(std::integral_constant<int, WC_CODE_INT8>{}) : with(std::integral_constant<int, WC_CODE_E4M3>{});
+        if (e != cudaSuccess) return e;
+        q_ctas = 0;   // with the first heads
+    }
+    return cudaSuccess;
 }
 
 }  // namespace wc

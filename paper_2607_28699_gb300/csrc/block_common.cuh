@@ -29,6 +29,7 @@ struct BlockAppendParams {
     uint32_t* dev_status;      // optional
     int32_t n_tok, batch, max_pages, num_pages, num_q_heads, num_kv_heads, num_positions, rotary_dim;
     int32_t page_tasks;        // upper bound of the pages written, over all sequences
+    int32_t page_head0, page_heads;   // KV heads of a launch
     int32_t page_ctas;         // CTAs of the page tasks, the first of every page_stride; the others rotate queries
     int32_t page_stride;
     int32_t q_heads;           // query heads of one token that a warp takes
