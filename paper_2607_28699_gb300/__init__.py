@@ -706,6 +706,8 @@ def qk_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positio
         if positions is None:
             raise ValueError("cos and sin need positions")
         rotary_dim, tables = 2 * shape[1], (_ints(positions, n_tok, "positions"), cos.data_ptr(), sin.data_ptr(), shape[0])
+    elif sin is not None or positions is not None:
+        raise ValueError("sin and positions need cos")
     st = lib.wc_qk_norm_rotate(act, out_act, *q_rows, *k_rows, n_tok, _weights(q_norm, "q_norm"), _weights(k_norm, "k_norm"), norm_eps, rope_layout,
                                rotary_dim, *tables, _ptr(dev_status), _stream(stream))
     if st:
