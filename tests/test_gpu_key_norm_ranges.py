@@ -7,6 +7,7 @@ import torch
 
 import _block_ref as R
 import _norm_ref as N
+from test_gpu_qk_norm import append_case
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +104,22 @@ def test_rows_past_the_range_are_lost_alone():
     i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
     wc.block_append(desc, g, g, i32(12), i32(1)[None], cache, cu_new=i32(0, 12), k_norm=torch.from_numpy(WEIGHT).cuda())
     assert torch.isnan(cache.k_scale.view(2, 2)[1]).all()
+
+
+@pytest.mark.parametrize("code", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("decode_form", [False, True])
+def test_among_usual_rows(code, interleaved, decode_form, monkeypatch):
+    """Such rows on pages with usual and older ones, rotated, packed; appended twice.  Rows whose sum of squares passes fp32's range are
+    NaN by definition, which the plain form in float64 does not have of itself."""
+    plain = N.norm
+    monkeypatch.setattr(N, "norm", lambda x, w, eps: np.where((x.astype(np.float64) ** 2).sum(-1, keepdims=True) < 2.0 ** 128, plain(x, w, eps), np.float32(np.nan)))
+
+    def edit(x, hq, hkv):
+        keys = x[:, hq:hq + hkv]
+        keys[::5] *= 2.0 ** 57
+        keys[3::7, 0] = 0
+        keys[3::7, 0, 9] = 1.3125 * 2.0 ** 63
+        keys[4::9, 1] *= 2.0 ** -66
+    ctx, new = ([60, 35, 17, 1, 16], [57, 20, 1, 1, 0]) if not decode_form else ([60, 35, 17, 1, 16, 33, 64] * 2, [1] * 14)
+    append_case(5, code, torch.bfloat16, ctx, new, hkv=3, hq=6, interleaved=interleaved, edit=edit, packed=True, decode_form=decode_form, batches=2)
