@@ -557,7 +557,7 @@ wc_status wc_block_append(const wc_block_desc* desc, int32_t act_type,
  *   y = (x r) w,  r = fp32(1 / sqrt(mean of x^2 over the 128 channels + norm_eps)),
  * w the 128 weights of k_norm (q_norm).  Keys: r is the fp32 nearest to its formula but for about one row in a
  * million (its neighbour then), the products and the rotation's are rounded to fp32 one by one, so that scales and
- * codes do not depend on the order of a sum.  Queries: in fp32 (to 2^-20 of the row's largest), rounded once to
+ * codes do not depend on the order of a sum.  Queries: in fp32 (to 22 x 2^-24 of the row's largest), rounded once to
  * act_type.  A row with infinities or NaN, or whose sum of squares passes fp32's range (bf16 values from 2^60 on),
  * becomes NaN (rows of k: the page's scale is NaN, as above).
  *   k_norm, q_norm  [128] fp32, device, 16-byte aligned, the same for every head; NULL: rows are not normed, and

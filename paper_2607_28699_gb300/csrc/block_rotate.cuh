@@ -213,8 +213,8 @@ __device__ __forceinline__ void scale_part(const float* weight, int a, int b, in
 
 // ---- for rows that are stored in 16 bits ---------------------------------------------------------
 
-// The factor of a row as norm_factor's but for rounding: sums of squares in fp32 (8 terms a half of a lane, then 4 sums of
-// two: 2^-20), where no code hangs on it.
+// The factor of a row as norm_factor's but for rounding, where no code hangs on it: sums of squares in fp32 (8 terms a half of a
+// lane, then 4 sums of two: 12 x 2^-24), half of that and 2 x 2^-24 in the root.
 template <bool kBf16>
 __device__ __forceinline__ float quick_factor(const Raw& raw, float eps) {
     const uint32_t w[8] = {raw.a.x, raw.a.y, raw.a.z, raw.a.w, raw.b.x, raw.b.y, raw.b.z, raw.b.w};
