@@ -4,16 +4,17 @@
 // lane's loads are 16 bytes.  A warp takes four rows at a time.  A page's rows are turned twice, for its amax and for its codes,
 // and loaded again for the second time (from L1): kept in registers they would take a quarter of the SM's warps, as fp32 half.
 // CTAs of pages lie among those that rotate queries: a page is a chain of loads, which the others' bytes hide (a 32k prompt
-// 95 us; pages first, then queries: 103).
+// 95 us; pages first, then queries: 103).  Normed queries and others have a loop each (with
+// norms 106.5 us; one loop for both 114.5).
 //
 // The norm of keys is summed in two floats (block_rotate.cuh): scales and codes hang on the factor's last bit.  With the norm the
-// page's loops are not unrolled: its instructions would stop fitting the cache (a 32k prompt 143 us instead of 121, measured on an
-// earlier form); what the loop will load is asked for ahead (118 us without the prefetches, 114.5 with).
+// page's loops are not unrolled: its instructions would stop fitting the cache (a 32k prompt 143 us instead of 121); what the loop
+// will load is asked for ahead (118 us without the prefetches, 114.5 with).  Both were measured on earlier forms.
 //
-// GB300, 28 query / 4 KV heads: a prompt of 32768 tokens 95 us, 6.2 TB/s of the 587 MB that it has to move (0.91 of the
-// measured copy rate), 16 ragged chunks of up to 1023 tokens (40 / 8 heads) 37 us; with norms 114.5 (0.75) and 48 us: its
-// 82 million warp instructions take 58% of the issue slots, its warps wait for loads for half of their time; one token 6 us, all of
-// it launch and a chain of four loads (context, block table, scale; rows and angles beside them).
+// GB300, 28 query / 4 KV heads: a prompt of 32768 tokens 94 us, 6.3 TB/s of the 587 MB that it has to move (0.92 of the
+// measured copy rate), 16 ragged chunks of up to 1023 tokens (40 / 8 heads) 37 us; with norms 106.5 (0.81) and 44 us: its
+// 77 million warp instructions take 59% of the issue slots, its warps wait for loads for half of their time; one token 3 us in a row
+// of calls, 9 by itself, all of it launch and a chain of four loads (context, block table, scale; rows and angles beside them).
 #include "block_rotate.cuh"
 
 namespace wc {
@@ -108,8 +109,8 @@ __device__ __noinline__ void append_wide_page(const BlockAppendParams& p) {
     append_page<kCode, kBf16, kHalfLayout, Norm::kWide>(p, (int)w.task, w.head, w.side);
 }
 
-// One warp: the new rows of one page and KV head, keys (side 0) or values.  A lane holds its channels of every
-// fourth row, so the page's amax is one warp reduction and the rows are read once.
+// One warp: the new rows of one page and KV head, keys (side 0) or values.  A lane takes its channels of every
+// fourth row, so the page's amax is one warp reduction.
 template <int kCode, bool kBf16, bool kHalfLayout, Norm kOf>
 __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task, int head, int side) {
     constexpr bool kNorm = kOf != Norm::kNone;
@@ -182,8 +183,7 @@ __device__ __forceinline__ void append_page(const BlockAppendParams& p, int task
         }
         if (at.rotated(part)) rotate<kHalfLayout>(trig, y);
     };
-    // The page's amax, then its codes: rows are loaded again (from L1) and turned again, since kept they would take the registers
-    // of a third of the warps, or of half as fp32.
+    // The page's amax, then its codes: rows are loaded again (from L1) and turned again.
     uint32_t mine = 0;             // bit j: step j has a row of this lane
     float most = 0.0f;
     float factors = 1.0f;          // lane i: of step i

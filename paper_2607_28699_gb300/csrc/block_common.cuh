@@ -133,7 +133,9 @@ __device__ __forceinline__ uint16_t float_to_act(float x, bool bf16) {
 // fp16's range), and the sum of weights holds what is above 2^(log2(s) - 53) of its own.
 constexpr float kLeastValueScale = 0x1p-100f, kNoValueScale = 0x1p-80f;
 
-// Weights 2^(y - m) are rounded to fp16 for the second product.  The frame m is put kHeadroom below the largest y, and moves
+// Weights 2^(y - m) are rounded to fp16 for the second product, whose operands on the tensor cores have 16 bits: at most 2^-11 of the
+// sum of p |v| (as much as fp16 outputs' own rounding: the error against 64 bits grows by 1.1 to 1.4 there, with bf16 outputs
+// not at all), where two fp16 parts a weight would double that product.  The frame m is put kHeadroom below the largest y, and moves
 // when one passes it by kTopWeight: the largest weight lies in [2^7, 2^15], and others keep all their bits down to 2^-21
 // of it, some to 2^-32 (from 1 on: 2^-14 and 2^-25, and what a sharp head gives to many tokens in all was lost below).  2^15
 // leaves fp16's range a factor of 2 for what fp32 rounds off exponents: those of logits up to 2^22.

@@ -14,14 +14,15 @@
 // that reaches over several leave partial results, and the last of them to arrive merges these
 // (in the order of the pages, so the result does not depend on which one it is).
 //
-// GB300, 4 KV heads of 7 query heads: 32 sequences of 4k to 32k 106 us (5.7 TB/s, 0.84 of the measured copy rate: the
-// page loop reads 7 TB/s, the rest is the first pages' latency and the merges), 16 of 4k to 8k 33 us, one of 32k 20 us
-// (6 us page loop at the copy rate; launch and block table before it, merges in the CTA and over 38 CTAs after it).
+// GB300, 4 KV heads of 7 query heads, a call by itself: 32 sequences of 4k to 32k 106 us (5.7 TB/s, 0.84 of the measured copy rate:
+// the page loop reads 7 TB/s, the rest is the first pages' latency and the merges), 16 of 4k to 8k 33 us, one of 32k 20 us
+// (6 us page loop at the copy rate; launch and block table before it, merges in the CTA and over 38 CTAs after it).  In a row of
+// calls, whose launches overlap, 102, 28 and 16 us (what fits the L2 read from there; with other inputs each time 31 and 19).
 // 16 warps on one CTA an SM (with three pages in flight each: 111 / 35 / 20.5 us; 8 warps on two CTAs 110 / 35 / 26, twice the
 // partial results; on one 131 / 37 / 23); several shares per SM, taken as SMs come free, 121 / 45 / 41 (each has its own
 // prologue and merge).
-// With a window of 4096 tokens and 64 sinks, 32 sequences 30 us (4.6 TB/s: 128 CTAs with a sequence and head each, whole
-// units; 12 us are launch, first pages and the merge in the CTA), 16 with a window of 1000 12 us, one with 512 9 us.
+// With a window of 4096 tokens and 64 sinks, in a row of calls, 32 sequences 30 us (4.5 TB/s: 128 CTAs with a sequence and head
+// each, whole units; 12 us are launch, first pages and the merge in the CTA), 16 with a window of 1000 12 us, one with 512 9 us.
 #include "block_common.cuh"
 #include "decode_common.cuh"
 
@@ -38,11 +39,17 @@ constexpr int kStageBytes = 2 * kPageBytes;
 constexpr int kRow = kHeadDim + 4;                     // floats of a merge row in shared memory
 constexpr int kMinPages = 1;                           // per warp, before a launch takes more CTAs
 constexpr float kNoMax = -3e38f;                       // the frame before the first logit
-// The units of windowed calls have about as many pages each.  Shares of whole units need no merges between CTAs; they are
-// taken where the longest is at most this many pages above an equal share (28 / 4 heads, 16 sequences of 64 pages, 37 above: 12.1 us
-// instead of 14.4; 32 of 261, 41 above: 29.8 instead of 33.9; 4 of 66, 50 above: 11.9 instead of 12.5, but 1 of 66, 50 above:
-// 11.5 instead of 10.1; 24 of 258, 95 above: 28.5 instead of 26.6).  The kernel finds it from the lengths (0.2 us): by the
-// window alone one sequence of 258 pages among 31 of 2 would have a CTA to itself (26.7 us instead of 16.0).
+// The units of windowed calls have about as many pages each.  Shares of whole units need no merges between CTAs, but leave SMs
+// without work; they are taken where the longest is at most this many pages above an equal share.  Whole against cut shares, us in a
+// row of calls (28 / 4 heads, 38 shares a head, units of n sequences; pages above):
+//   window 1024   n 1 (52) 11.9 / 10.3   4 (50) 12.2 / 12.8   12 (45) 12.3 / 13.9   16 (38) 12.3 / 14.3
+//   window 2048   n 16 (75) 17.6 / 16.4  20 (62) 17.6 / 18.1  24 (48) 17.7 / 18.9   27 (38) 17.7 / 19.5
+//   window 4096   n 24 (95) 29.1 / 26.7  28 (68) 29.7 / 29.8  31 (48) 30.4 / 33.5   32 (41) 30.4 / 34.0
+//   window 8192   n 27 (149) 51.8 / 47.8 31 (95) 51.9 / 54.7  36 (27) 53.0 / 59.4
+// Up to 41 above whole shares were never behind.  What the merges cost grows with sequences and pages, so one number has to miss some:
+// at 44 one or two short units stay cut (1.6 us), and 28 to 31 sequences of 4096 too, which lose up to 3.1 us by it.  The kernel finds
+// the shares from the lengths (0.2 us): by the window alone one sequence of 258 pages among 31 of 2 would have a CTA to itself (26.7
+// us instead of 16.0).
 constexpr int kWholePages = 44;
 
 struct DecodeArgs {

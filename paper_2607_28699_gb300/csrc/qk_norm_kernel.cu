@@ -7,7 +7,8 @@
 //
 // GB300, 28 query / 4 KV heads, 32768 tokens, fp16: 82 us, 6.75 TB/s of the 554 MB that it has to move (0.99 of the measured
 // copy rate).  Tried: steps fetched two at a time, both written before the next two (86 us), three ahead with 24 warps an SM
-// (90), four with 24 and spilled rows (89); 32 tokens of 32 heads 2.4 us between launches.
+// (90), four with 24 and spilled rows (89); 32 tokens of 32 heads 2.5 us between launches.  Rows without a
+// norm have a path of their own.
 #include "block_rotate.cuh"
 
 namespace wc {
